@@ -239,12 +239,17 @@ def _table_lengths(case):
     return length, new
 
 
+def _table_pages(length, new):
+    """Pages of every sequence (every third has one to spare, that a rejected draft left behind) and how many it misses."""
+    held = [-(-p // PAGE) + (i % 3 == 2) for i, p in enumerate(length)]
+    return held, [max(0, -(-(p + n) // PAGE) - h) for p, n, h in zip(length, new, held)]
+
+
 def _prepare_table(case, g, st):
     length, new = _table_lengths(case)
     B = case["batch"]
-    pps = max(-(-(p + n) // PAGE) for p, n in zip(length, new)) + 1
-    held = [-(-p // PAGE) for p in length]
-    need = [-(-(p + n) // PAGE) - h for p, n, h in zip(length, new, held)]
+    pps = max(-(-(p + n) // PAGE) for p, n in zip(length, new)) + 2
+    held, need = _table_pages(length, new)
     n_free = max(1, sum(need) * 9 // 10) if case["short"] else sum(need) + 5
     n_pages = sum(held) + n_free + 4096                    # the rest belongs to nobody here
     ids = torch.randperm(n_pages, generator=g, device=DEV).to(torch.int32)
@@ -253,7 +258,7 @@ def _prepare_table(case, g, st):
     table = torch.where(torch.arange(pps, device=DEV) < h[:, None], ids[at.clamp(max=n_pages - 1)], -1).to(torch.int32)
     i32 = {"dtype": torch.int32, "device": DEV}
     st.update(lens=torch.tensor(length, **i32), new=torch.tensor(new, **i32), free=ids[sum(held):sum(held) + n_free].contiguous(), table=table,
-              n_pages=n_pages, start=torch.empty(B + 1, **i32), slots=torch.empty(sum(new) + 3, **i32),
+              n_pages=n_pages, held=torch.tensor(held, **i32), held_out=torch.empty(B, **i32), start=torch.empty(B + 1, **i32), slots=torch.empty(sum(new) + 3, **i32),
               granted=torch.empty(B, **i32), taken=torch.empty(1, **i32))
     if own:
         import paper_2511_08923_amd as T
@@ -273,9 +278,9 @@ def _own(st):
     import paper_2511_08923_amd as T
     c = st["case"]
     if c["kind"] == "table":
-        T.tidar_table_extend(st["ctx"], c["batch"], st["lens"], st["new"], st["free"], st["free"].numel(), st["table"],
-                             st["n_pages"], st["start"], st["slots"], st["granted"], st["taken"])
-        return {k: st[k] for k in ("table", "start", "slots", "granted", "taken")}
+        T.tidar_table_extend(st["ctx"], c["batch"], st["lens"], st["new"], st["held"], st["free"], st["free"].numel(), st["table"],
+                             st["n_pages"], st["start"], st["slots"], st["held_out"], st["granted"], st["taken"])
+        return {k: st[k] for k in ("table", "start", "slots", "held_out", "granted", "taken")}
     if c["kind"] == "store":
         T.tidar_kv4_store(st["ctx"], st["kv4"], 0, c["rows"], st["slots"], st["k"], st["v"])
         T.tidar_kv4_load(st["ctx"], st["kv4"], 0, c["rows"], st["slots"], st["k_out"], st["v_out"])
@@ -293,8 +298,8 @@ def _own(st):
 def _plain_table(st):
     P, n, table, free = st["lens"].long(), st["new"].long(), st["table"], st["free"]
     B, pps = table.shape
-    held = (P + PAGE - 1) // PAGE
-    need = (P + n + PAGE - 1) // PAGE - held
+    held = st["held"].long()
+    need = ((P + n + PAGE - 1) // PAGE - held).clamp(min=0)
     off, end = need.cumsum(0) - need, n.cumsum(0)
     ok = (need == 0) | (off + need <= free.numel())                                 # nothing needed, nothing to wait for
     j = torch.arange(pps, device=DEV)
@@ -307,7 +312,8 @@ def _plain_table(st):
     slots = torch.where(ok[b] & (r < end[-1]), table[b, pos // PAGE] * PAGE + pos % PAGE, -1).to(torch.int32)
     start = torch.cat((torch.zeros_like(end[:1]), end)).to(torch.int32)
     taken = torch.where(ok & (need > 0), off + need, 0).amax().view(1).to(torch.int32)
-    return {"table": table, "start": start, "slots": slots, "granted": ok.to(torch.int32), "taken": taken}
+    now = torch.where(ok, held + need, held).to(torch.int32)
+    return {"table": table, "start": start, "slots": slots, "held_out": now, "granted": ok.to(torch.int32), "taken": taken}
 
 
 def _plain_store(st):
@@ -378,8 +384,8 @@ def _pairs(case):
 def work(case):
     if case["kind"] == "table":
         length, new = _table_lengths(case)
-        taken = sum(-(-(p + n) // PAGE) - -(-p // PAGE) for p, n in zip(length, new))
-        return {"bytes": 4 * (3 * len(new) + 2 * taken + 2 * len(new) + 1 + sum(new) + 4), "flops": 0}
+        taken = sum(_table_pages(length, new)[1])
+        return {"bytes": 4 * (4 * len(new) + 2 * taken + 3 * len(new) + 1 + sum(new) + 4), "flops": 0}
     n_q, n_kv, hd = HEADS[case["heads"]]
     size = 2 if case["dtype"] == "bf16" else 4
     row4 = n_kv * (hd // 2 + hd // 32)
