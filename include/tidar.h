@@ -292,6 +292,107 @@ tidar_status tidar_score(tidar_ctx *ctx, const tidar_weights *w, const tidar_kv_
                          float *ar_logprob, float *diff_logprob, float *loss, void *ws, size_t ws_bytes,
                          void *stream);
 
+/*
+ * ---- Around the cache: page tables from request lengths, a cache in 4 bits, attention over a span.
+ *
+ * A *slot* names one position of the pool: slot = page id * 16 + offset in the page.  Slots, page ids and lengths of
+ * these calls are int32, so a pool has at most 2^27 pages and a table at most 2^26 pages per sequence (more: TIDAR_EINVAL).
+ * Unlike the calls above, nothing here limits the bytes of a layer's 4-bit pages.  Pages, q, out and ws must be
+ * 16-byte aligned (TIDAR_EINVAL).
+ */
+
+/*
+ * Page table entries and slots for the rows that every sequence is about to get (a prompt's chunk, a draft, one token).
+ * Sequence b holds positions [0, prefix_len[b]), its row of the table has held[b] pages (also such as rejected drafts left
+ * behind), and it gets n_new[b] rows at prefix_len[b].  The pages that are missing, entries held .. ceil((prefix_len + n_new)/16) - 1,
+ * are taken from the free list in the order of the sequences; no other entry is written.  The new rows of all sequences are numbered one after another:
+ * sequence b has rows row_start[b] .. row_start[b + 1] - 1, and slots[] holds where each goes.
+ *   prefix_len, n_new, held   dev int32 [batch]; prefix_len is not changed (the attention calls take the same)
+ *   free_pages  dev int32 [n_free]: ids of free pages, each once (NULL with n_free 0); the list is not changed
+ *   page_table  dev int32 [batch][pages_per_seq] in/out
+ *   row_start   dev int32 [batch + 1] out (a sum beyond 2^31 - 1 reads 2^31 - 1)
+ *   slots       dev int32 [slot_cap] out; -1 for the rows of a sequence that was not granted, and behind the last row
+ *   held_out    dev int32 [batch] out: pages of the sequence now (held where it is not granted), for the next call; an array of its own
+ *               (one that overlaps held is refused: sequences read the held of those before them while theirs is written)
+ *   granted     dev int32 [batch] out: 1, or 0 where the free list ends before the sequence's last page or its rows do not
+ *               end within slot_cap, or -1 where its lengths (negative, beyond pages_per_seq * 16, or more positions
+ *               than its pages hold), a page that its rows go into or a page id of its part of the list is not valid.  A sequence that is not granted gets no page and no slot, and
+ *               nothing of its row of the table is written; it may be tried again.  Sequences do not overtake: behind one that the
+ *               list was too short for, only those are granted that need no page.
+ *   n_taken     dev int32 [1] out: entries of the free list that are used up, from its beginning (the part of a sequence
+ *               that is refused for an invalid id counts among them)
+ * n_new outside [0, pages_per_seq * 16] counts as no rows.
+ */
+tidar_status tidar_table_extend(tidar_ctx *ctx, int32_t batch, const int32_t *prefix_len, const int32_t *n_new,
+                                const int32_t *held, const int32_t *free_pages, int32_t n_free, int32_t *page_table,
+                                int32_t pages_per_seq, int32_t n_pages, int32_t *row_start, int32_t *slots,
+                                int32_t slot_cap, int32_t *held_out, int32_t *granted, int32_t *n_taken, void *stream);
+
+/*
+ * Paged KV cache in 4 bits: a quarter of the bytes of the exact bf16 cache, 27 % with its scales.
+ *   pages : [n_layers][n_pages][n_kv_heads][544 * nb bytes], nb = ceil(head_dim / 32); tidar_kv4_page_bytes is one layer's page of
+ *           all heads.  A head's block holds, one after another,
+ *             K codes  [nb][16 tokens][16 bytes]: byte j = elements 2j (low 4 bits) and 2j + 1 of the 32-element block
+ *             V codes  [4][4 nb][4 tokens][4 bytes]: token quad, group of 8 elements, token, byte j = elements 2j, 2j + 1
+ *             K scales [nb][16 tokens], V scales [nb][16 tokens]: one byte per token and block
+ *   page_table, pages_per_seq : as in tidar_kv_cache (tidar_kv4_store and tidar_kv4_load do not read them)
+ * An element is code * 2^(scale - 127); codes are 0, 1/2, 1, 3/2, 2, 3, 4, 6 with a sign in bit 3.  A block's scale is the
+ * smallest power of two of which its largest magnitude is at most 7 times (2 <= scale <= 252), every element goes to the nearest code,
+ * ties to the even one, so no element is off by more than half of the distance between its neighbours.  A block that holds an
+ * infinity or NaN reads back as NaN (scale 255).
+ */
+typedef struct {
+    void *pages;
+    const int32_t *page_table;
+    int32_t pages_per_seq;
+    int32_t n_pages;
+} tidar_kv4_cache;
+size_t       tidar_kv4_page_bytes(const tidar_ctx *ctx);
+
+/*
+ * Rows of K (after RoPE) and V into 4-bit pages, and back as the values that are held.
+ *   slots  dev int32 [n_rows]; a slot outside [0, n_pages * 16) (-1: padding) stores nothing and reads 0.  A slot named by two
+ *          rows of one store holds neither for certain.
+ *   k, v   dev [n_rows][n_kv_heads][head_dim], config dtype
+ * n_rows may be 0.
+ */
+tidar_status tidar_kv4_store(tidar_ctx *ctx, const tidar_kv4_cache *kv, int32_t layer, int32_t n_rows,
+                             const int32_t *slots, const void *k, const void *v, void *stream);
+tidar_status tidar_kv4_load(tidar_ctx *ctx, const tidar_kv4_cache *kv, int32_t layer, int32_t n_rows,
+                            const int32_t *slots, void *k, void *v, void *stream);
+
+/*
+ * tidar_hybrid_attention with a sliding window and sinks: rows, mask and K/V of the new rows as there, and of the keys a
+ * row at position p sees under that mask only those at positions > p - window or < sinks (a mask row's own block
+ * included, by the positions its rows stand for).  window >= 1: a row always sees itself; sinks >= 0.
+ * Pages wholly outside a sequence's sinks and windows are not read, and neither are their table entries: they may be
+ * given to other sequences.  What a masked place holds (stale slots, infinities, NaN) has no influence.
+ * A sequence whose prefix_len is not valid gets NaN in all its rows, and nothing of it is stored; a page id that is not valid
+ * gives NaN to the rows that see its page, and possibly to other rows of the sequence.
+ */
+tidar_status tidar_window_attention(tidar_ctx *ctx, const tidar_kv_cache *kv, int32_t layer, int32_t batch,
+                                    const int32_t *prefix_len, const void *q, const void *k_new, const void *v_new,
+                                    int32_t n_causal, int32_t n_blocks, int32_t block_len, int32_t cond0, int32_t window,
+                                    int32_t sinks, void *out, int32_t max_prefix_len_hint, void *ws, size_t ws_bytes,
+                                    void *stream);
+
+/*
+ * The hybrid-mask attention over the cache in 4 bits.  It only reads the cache: the causal rows' K/V have been
+ * stored at positions prefix_len[b] .. prefix_len[b] + n_causal - 1 before (tidar_kv4_store), and every row of the call,
+ * the causal row itself among them, sees them as they are held.  Mask rows are never cached; theirs are read as they are:
+ *   k_mask, v_mask  dev [batch][n_blocks * block_len][n_kv_heads][head_dim] (NULL with n_blocks 0)
+ * window 0: no window (sinks must be 0 then); otherwise as in tidar_window_attention, and so are invalid lengths and page ids.
+ */
+tidar_status tidar_kv4_attention(tidar_ctx *ctx, const tidar_kv4_cache *kv, int32_t layer, int32_t batch,
+                                 const int32_t *prefix_len, const void *q, const void *k_mask, const void *v_mask,
+                                 int32_t n_causal, int32_t n_blocks, int32_t block_len, int32_t cond0, int32_t window,
+                                 int32_t sinks, void *out, int32_t max_prefix_len_hint, void *ws, size_t ws_bytes,
+                                 void *stream);
+
+/* Workspace of either for up to `batch` sequences with these rows, prefixes up to max_prefix_len and any window. */
+tidar_status tidar_attention_workspace_bytes(const tidar_ctx *ctx, int32_t batch, int32_t n_causal, int32_t n_blocks,
+                                             int32_t block_len, int32_t max_prefix_len, size_t *bytes);
+
 /* Causal rows per prefill pass (the prompt is prefilled in causal chunks through the step's kernels, the mask block
  * of Appendix B joins the last chunk).  Default 2048; 1..4096.  Larger passes stream the weights fewer times and
  * need a larger workspace: call before tidar_workspace_bytes / tidar_score_workspace_bytes.  Host only. */

@@ -28,7 +28,8 @@ EXPORTS = ["tidar_create", "tidar_destroy", "tidar_strerror", "tidar_packed_weig
            "tidar_workspace_bytes", "tidar_prefill", "tidar_step", "tidar_ar_step", "tidar_hybrid_attention",
            "tidar_gemm_workspace_bytes", "tidar_gemm", "tidar_profile_enable", "tidar_profile_read",
            "tidar_profile_reset", "tidar_select_block_len", "tidar_set_prefill_chunk", "tidar_score_workspace_bytes",
-           "tidar_score", "tidar_gemm_static"]
+           "tidar_score", "tidar_gemm_static", "tidar_table_extend", "tidar_kv4_page_bytes", "tidar_kv4_store",
+           "tidar_kv4_load", "tidar_kv4_attention", "tidar_window_attention", "tidar_attention_workspace_bytes"]
 STATIC_SCRATCH_BYTES = 32 << 20
 
 
@@ -54,6 +55,10 @@ class tidar_weights(C.Structure):
 class tidar_kv_cache(C.Structure):
     _fields_ = [("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("page_table", C.c_void_p),
                 ("pages_per_seq", C.c_int32), ("n_pages", C.c_int32)]
+
+
+class tidar_kv4_cache(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("page_table", C.c_void_p), ("pages_per_seq", C.c_int32), ("n_pages", C.c_int32)]
 
 
 class tidar_mode(C.Structure):
@@ -110,6 +115,18 @@ def _load() -> C.CDLL:
     lib.tidar_score.argtypes = [vp, C.POINTER(tidar_weights), C.POINTER(tidar_kv_cache), i32, vp, i32, C.POINTER(i32),
                                 i32, C.c_float, vp, vp, vp, vp, sz, vp]
     lib.tidar_score.restype = i32
+    lib.tidar_table_extend.argtypes = [vp, i32, vp, vp, vp, vp, i32, vp, i32, i32, vp, vp, i32, vp, vp, vp, vp]
+    lib.tidar_table_extend.restype = i32
+    lib.tidar_kv4_page_bytes.argtypes = [vp]
+    lib.tidar_kv4_page_bytes.restype = sz
+    for f in (lib.tidar_kv4_store, lib.tidar_kv4_load):
+        f.argtypes = [vp, C.POINTER(tidar_kv4_cache), i32, i32, vp, vp, vp, vp]
+        f.restype = i32
+    for f, cache in ((lib.tidar_window_attention, tidar_kv_cache), (lib.tidar_kv4_attention, tidar_kv4_cache)):
+        f.argtypes = [vp, C.POINTER(cache), i32, i32, vp, vp, vp, vp, i32, i32, i32, i32, i32, i32, vp, i32, vp, sz, vp]
+        f.restype = i32
+    lib.tidar_attention_workspace_bytes.argtypes = [vp, i32, i32, i32, i32, i32, C.POINTER(sz)]
+    lib.tidar_attention_workspace_bytes.restype = i32
     return lib
 
 
@@ -129,9 +146,15 @@ def _stream() -> int:
     return torch.cuda.current_stream().cuda_stream
 
 
+class tidar_ctx(C.c_void_p):
+    """The library's handle; carries the configuration it was made from."""
+    cfg: tidar_config
+
+
 # ---------------------------------------------------------------- functions named after the C entry points
-def tidar_create(cfg: tidar_config) -> C.c_void_p:
-    h = C.c_void_p()
+def tidar_create(cfg: tidar_config) -> tidar_ctx:
+    h = tidar_ctx()
+    h.cfg = cfg
     _check(_lib.tidar_create(C.byref(cfg), C.byref(h)), "tidar_create")
     return h
 
@@ -237,6 +260,94 @@ def tidar_score(ctx, w: tidar_weights, kv: tidar_kv_cache, batch: int, tokens: t
     _check(_lib.tidar_score(ctx, C.byref(w), C.byref(kv), batch, tokens.data_ptr(), tokens.shape[1], lens, block_len,
                             alpha, ar_logprob.data_ptr(), _ptr(diff_logprob), _ptr(loss), ws.data_ptr(),
                             ws.numel() * ws.element_size(), _stream()), "tidar_score")
+
+
+# The calls around the cache check their tensors: a view with other strides, another type or device, or one that is too small
+# is refused (ValueError) before anything is enqueued.
+_DTYPE = {TIDAR_F32: torch.float32, TIDAR_BF16: torch.bfloat16}
+
+
+def _mem(name: str, t: torch.Tensor, dtype: Optional[torch.dtype], numel: int) -> int:
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{name}: {t.dtype}, expected {dtype}")
+    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{name}: on {t.device}, expected the current GPU")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: not contiguous (strides {tuple(t.stride())})")
+    if t.numel() < numel:
+        raise ValueError(f"{name}: {t.numel()} elements, expected at least {numel}")
+    return t.data_ptr()
+
+
+def tidar_table_extend(ctx: tidar_ctx, batch: int, prefix_len: torch.Tensor, n_new: torch.Tensor, held: torch.Tensor,
+                       free_pages: Optional[torch.Tensor], n_free: int, page_table: torch.Tensor, n_pages: int,
+                       row_start: torch.Tensor, slots: torch.Tensor, held_out: torch.Tensor, granted: torch.Tensor,
+                       n_taken: torch.Tensor) -> None:
+    i32, pps = torch.int32, page_table.shape[-1]
+    _check(_lib.tidar_table_extend(ctx, batch, _mem("prefix_len", prefix_len, i32, batch), _mem("n_new", n_new, i32, batch),
+                                   _mem("held", held, i32, batch),
+                                   None if free_pages is None else _mem("free_pages", free_pages, i32, n_free), n_free,
+                                   _mem("page_table", page_table, i32, batch * pps), pps, n_pages,
+                                   _mem("row_start", row_start, i32, batch + 1), _mem("slots", slots, i32, 0), slots.numel(),
+                                   _mem("held_out", held_out, i32, batch), _mem("granted", granted, i32, batch), _mem("n_taken", n_taken, i32, 1), _stream()),
+           "tidar_table_extend")
+
+
+def tidar_kv4_page_bytes(ctx: tidar_ctx) -> int:
+    return int(_lib.tidar_kv4_page_bytes(ctx))
+
+
+def _kv4_rows(fn, where: str, ctx: tidar_ctx, kv, layer: int, n_rows: int, slots, k, v) -> None:
+    c = ctx.cfg
+    dt, n = _DTYPE[c.dtype], n_rows * c.n_kv_heads * c.head_dim
+    _check(fn(ctx, C.byref(kv), layer, n_rows, _mem("slots", slots, torch.int32, n_rows), _mem("k", k, dt, n),
+              _mem("v", v, dt, n), _stream()), where)
+
+
+def tidar_kv4_store(ctx: tidar_ctx, kv: tidar_kv4_cache, layer: int, n_rows: int, slots: torch.Tensor, k: torch.Tensor,
+                    v: torch.Tensor) -> None:
+    _kv4_rows(_lib.tidar_kv4_store, "tidar_kv4_store", ctx, kv, layer, n_rows, slots, k, v)
+
+
+def tidar_kv4_load(ctx: tidar_ctx, kv: tidar_kv4_cache, layer: int, n_rows: int, slots: torch.Tensor, k: torch.Tensor,
+                   v: torch.Tensor) -> None:
+    _kv4_rows(_lib.tidar_kv4_load, "tidar_kv4_load", ctx, kv, layer, n_rows, slots, k, v)
+
+
+def _span_attention(fn, where: str, ctx: tidar_ctx, kv, layer, batch, prefix_len, q, k_new, v_new, new_rows, n_causal,
+                    n_blocks, block_len, cond0, window, sinks, out, hint, ws) -> None:
+    c = ctx.cfg
+    dt, n_q = _DTYPE[c.dtype], batch * (n_causal + n_blocks * block_len) * c.n_q_heads * c.head_dim
+    n_kv = batch * new_rows * c.n_kv_heads * c.head_dim
+    _check(fn(ctx, C.byref(kv), layer, batch, _mem("prefix_len", prefix_len, torch.int32, batch), _mem("q", q, dt, n_q),
+              None if k_new is None else _mem("k", k_new, dt, n_kv), None if v_new is None else _mem("v", v_new, dt, n_kv),
+              n_causal, n_blocks, block_len, cond0, window, sinks, _mem("out", out, dt, n_q), hint, _mem("ws", ws, None, 0),
+              ws.numel() * ws.element_size(), _stream()), where)
+
+
+def tidar_window_attention(ctx: tidar_ctx, kv: tidar_kv_cache, layer: int, batch: int, prefix_len: torch.Tensor,
+                           q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor, n_causal: int, n_blocks: int,
+                           block_len: int, cond0: int, window: int, sinks: int, out: torch.Tensor, max_prefix_len_hint: int,
+                           ws: torch.Tensor) -> None:
+    _span_attention(_lib.tidar_window_attention, "tidar_window_attention", ctx, kv, layer, batch, prefix_len, q, k_new, v_new,
+                    n_causal + n_blocks * block_len, n_causal, n_blocks, block_len, cond0, window, sinks, out,
+                    max_prefix_len_hint, ws)
+
+
+def tidar_kv4_attention(ctx: tidar_ctx, kv: tidar_kv4_cache, layer: int, batch: int, prefix_len: torch.Tensor,
+                        q: torch.Tensor, k_mask: Optional[torch.Tensor], v_mask: Optional[torch.Tensor], n_causal: int,
+                        n_blocks: int, block_len: int, cond0: int, window: int, sinks: int, out: torch.Tensor,
+                        max_prefix_len_hint: int, ws: torch.Tensor) -> None:
+    _span_attention(_lib.tidar_kv4_attention, "tidar_kv4_attention", ctx, kv, layer, batch, prefix_len, q, k_mask, v_mask,
+                    n_blocks * block_len, n_causal, n_blocks, block_len, cond0, window, sinks, out, max_prefix_len_hint, ws)
+
+
+def tidar_attention_workspace_bytes(ctx, batch: int, n_causal: int, n_blocks: int, block_len: int,
+                                    max_prefix_len: int) -> int:
+    n = C.c_size_t()
+    _check(_lib.tidar_attention_workspace_bytes(ctx, batch, n_causal, n_blocks, block_len, max_prefix_len, C.byref(n)),
+           "tidar_attention_workspace_bytes")
+    return int(n.value)
 
 
 def tidar_profile_reset(ctx) -> None:

@@ -1,0 +1,636 @@
+// Hybrid-mask attention over a span of the paged cache: a sliding window and a few first tokens (sinks), or all of it, from
+// exact pages or 4-bit pages.
+//
+// The mask.  A row at position p sees the cache below its own bound (causal row r: L + r + 1; a row of mask block j: L + cond0
+// + j) and, a mask row, its own block.  With a window w and t sinks a key at position x is left out where x <= p - w, unless
+// x < t.  For one row the visible keys are thus two ranges of the cache, [0, sk) and [lo, hi), and two of the mask rows.
+//
+// The walk.  A workgroup takes a tile of 16 query rows of a kv head (the rows of all its query heads, head-major) and walks only the
+// units of 16 keys (cache pages, then mask tiles) that any of its rows sees; any two units make an iteration of 32 keys.  Pages
+// between the sinks and the window are never read, not even their table entries.  The four waves take every fourth iteration,
+// each with its own softmax state, straight from memory into registers (no LDS, no barrier in the loop), and are folded through
+// LDS at the end.  Where the tiles do not fill the chip the walk is cut into key splits, evenly by its real length, and the partial
+// results are joined by a second kernel.
+//
+// The softmax.  Scores are formed transposed, S^T[key][q], so that a lane holds one query row's scores of its keys and they are,
+// without moving, the B operand of O^T[d][q] += V^T[d][key] P^T[key][q].  Numerators are taken against a power of two that is
+// moved only when the scores outgrow it by 2^16 (and from -inf by a row's first key): every rescale is exact, and no common
+// path reduces a maximum across lanes.  (A reference may lag behind the waves' and splits' common maximum by the 2^16, and
+// what is folded with a factor below 2^-126 is lost: weights below 2^-110 of a row's largest.)  bf16: numerators are rounded to bf16 for the matrix product (relative 2^-9, as in
+// tidar_hybrid_attention) and the denominator sums the rounded values in fp32.
+//
+// What a masked place holds never shows: scores are replaced by -inf, and infinities and NaN of V, which a weight of zero would
+// turn into NaN, are taken out of the product in units that are not wholly visible, and put back for the rows that see them.
+#include <algorithm>
+#include <type_traits>
+
+#include "kv4_format.h"
+#include "tidar_internal.h"
+
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLag = 16.f;                             // log2 of how far scores may outgrow the softmax reference
+typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+
+struct SpanArgs {
+    SpanCall c;
+    int group, tiles, splits;
+    float *opart, *mpart, *lpart;
+};
+
+// What one query row sees: cache keys [0, sk) and [lo, hi), mask rows [m0, ms) and [ml, m1).
+struct RowSpan {
+    int lo, hi, sk;
+    int m0, ms, ml, m1;
+};
+__device__ inline RowSpan row_span(const RowDesc &d, int r, int L, int window, int sinks) {
+    const RowInfo ri = row_info(d, r, L);
+    RowSpan s;
+    s.hi = L + ri.vis;
+    s.lo = window > 0 ? max(0, ri.pos - window + 1) : 0;
+    s.sk = window > 0 ? min(sinks, s.hi) : 0;
+    s.m0 = s.ms = s.ml = s.m1 = 0;
+    if (ri.blk >= 0) {                                   // mask row m of the block sits at position hi + m - m0
+        s.m0 = ri.blk * d.bl;
+        s.m1 = min(s.m0 + d.bl, d.nm);
+        s.ml = max(s.m0, s.m0 + s.lo - s.hi);
+        s.ms = window > 0 ? min(s.m1, s.m0 + sinks - s.hi) : s.m0;
+    }
+    return s;
+}
+__device__ inline unsigned bits16(int lo, int hi) {      // bits [lo, hi) of 16
+    lo = min(max(lo, 0), 16);
+    hi = min(max(hi, 0), 16);
+    return hi > lo ? ((1u << hi) - 1u) & ~((1u << lo) - 1u) : 0u;
+}
+
+// The units a tile of rows walks: cache units [0, n_s), [w0, w0 + n_w), then mask units [um0, um0 + n_m).
+struct Walk {
+    int n_s, w0, n_w, um0, n_m;
+    int n1, n2;                                          // iterations over the cache and over the mask tiles
+    int lo_max, hi_min, sk_min;                          // of the rows: a unit within all of their ranges needs no mask
+};
+__device__ inline Walk make_walk(const RowSpan &s, bool row, int window) {
+    // over the 16 rows (lanes of the same q hold the same row)
+    int lo0 = row ? s.lo : 0x7fffffff, lo1 = row ? s.lo : 0, hi0 = row ? s.hi : 0x7fffffff, hi1 = row ? s.hi : 0;
+    int sk0 = row ? s.sk : 0x7fffffff, sk1 = row ? s.sk : 0;
+    const bool mask = row && s.m1 > s.m0;
+    int m0 = mask ? s.m0 : 0x7fffffff, m1 = mask ? s.m1 : 0;
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) {
+        lo0 = min(lo0, __shfl_xor(lo0, o));
+        lo1 = max(lo1, __shfl_xor(lo1, o));
+        hi0 = min(hi0, __shfl_xor(hi0, o));
+        hi1 = max(hi1, __shfl_xor(hi1, o));
+        sk0 = min(sk0, __shfl_xor(sk0, o));
+        sk1 = max(sk1, __shfl_xor(sk1, o));
+        m0 = min(m0, __shfl_xor(m0, o));
+        m1 = max(m1, __shfl_xor(m1, o));
+    }
+    Walk w;
+    auto uni = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
+    w.lo_max = uni(lo1);
+    w.hi_min = uni(hi0);
+    w.sk_min = uni(sk0);
+    w.n_s = uni(window > 0 ? (sk1 + 15) >> 4 : 0);
+    w.w0 = uni(lo0) >> 4;
+    const int w1 = (uni(hi1) + 15) >> 4;
+    if (w.n_s >= w.w0) {                                 // sinks and window meet
+        w.n_s = 0;
+        w.w0 = 0;
+    }
+    w.n_w = max(0, w1 - w.w0);
+    m0 = uni(m0);
+    m1 = uni(m1);
+    w.um0 = m1 > 0 ? m0 >> 4 : 0;
+    w.n_m = m1 > 0 ? ((m1 + 15) >> 4) - w.um0 : 0;
+    w.n1 = (w.n_s + w.n_w + 1) >> 1;
+    w.n2 = (w.n_m + 1) >> 1;
+    return w;
+}
+
+__device__ inline unsigned nonfinite2(unsigned x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+
+// T: bf16 (head_dim 128) or float; KV4: 4-bit pages; HT: head_dim tiles of 16.
+template <class T, bool KV4, int HT>
+__global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
+    constexpr bool BF = sizeof(T) == 2;
+    constexpr int HD = 16 * HT;                          // head_dim, padded to the tiles
+    constexpr int Q4 = HD / 4;                           // fp32: head-dim values of a lane's quarter
+    constexpr bool QUADS = !BF || KV4;                   // a lane's eight keys: two quads, or a run of eight
+    __shared__ float red[4][16][HD + 4];
+    __shared__ float m_lds[4][16], l_lds[4][16];
+    const SpanCall &c = a.c;
+    const RowDesc &d = c.d;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lq = lane & 15, kg = lane >> 4;
+    const int n_kv = KV4 ? c.kv4.n_kv : c.kv.n_kv, hd = BF ? HD : (KV4 ? c.kv4.hd : c.kv.hd);
+    const int pps = KV4 ? c.kv4.pages_per_seq : c.kv.pages_per_seq, n_pages = KV4 ? c.kv4.n_pages : c.kv.n_pages;
+    const int grp = blockIdx.x / a.tiles, tile = blockIdx.x - grp * a.tiles, split = blockIdx.y;
+    const int b = grp / n_kv, g = grp - b * n_kv;
+    const int F = a.group * d.R;
+    const int L_raw = c.prefix_len[d.seq_base + b];
+    const bool fits = L_raw >= 0 && (long long)L_raw + d.nc <= (long long)pps * 16;
+    const int L = fits ? L_raw : 0;
+    const int f = tile * 16 + lq;
+    const bool row = f < F;
+    const int hq = row ? f / d.R : 0, r = row ? f - hq * d.R : 0;
+    RowSpan rs = row_span(d, r, L, c.window, c.sinks);
+    const Walk wk = make_walk(rs, row, c.window);
+    if (!row) rs.hi = rs.lo = rs.sk = rs.m0 = rs.ms = rs.ml = rs.m1 = 0;
+    const int n_it = fits ? wk.n1 + wk.n2 : 0, per = (n_it + a.splits - 1) / a.splits;
+    const int it0 = min(n_it, split * per), it1 = min(n_it, it0 + per);
+    const __attribute__((address_space(4))) int32_t *pt = (const __attribute__((address_space(4))) int32_t *)(
+        (KV4 ? c.kv4.page_table : c.kv.page_table) + (size_t)(d.seq_base + b) * pps);
+    const int n_mt = (d.nm + 15) >> 4;
+    bool bad = !fits;                                    // a page id outside the pool: the rows come out as NaN
+
+    // ---- Q: B operand, lane = (row, quarter).  bf16 step s of 32: head-dim values 32 kg + 8 s .. (4-bit pages: a lane's
+    // quarter is one block) or 32 s + 8 kg .. ; fp32 step s of 4: value Q4 kg + s
+    const T *qp = (const T *)c.q + (((size_t)b * d.R + r) * c.n_q + (g * a.group + hq)) * hd;
+    bf16x8 qb[4];
+    float qf[BF ? 1 : Q4];
+    if constexpr (BF) {
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            qb[s] = (bf16x8){0, 0, 0, 0, 0, 0, 0, 0};
+            if (row) qb[s] = *(const bf16x8 *)(qp + (KV4 ? 32 * kg + 8 * s : 32 * s + 8 * kg));
+        }
+    } else {
+#pragma unroll
+        for (int s = 0; s < Q4; ++s) qf[s] = row && Q4 * kg + s < hd ? qp[Q4 * kg + s] : 0.f;
+    }
+    const float scale = kLog2e / sqrtf((float)hd);
+    f32x4 acc[HT];
+#pragma unroll
+    for (int t = 0; t < HT; ++t) acc[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    float m_run = -INFINITY, l_run = 0.f;
+
+    // the unit (or -1) of walk position w
+    auto cache_unit = [&](int w) { return w < wk.n_s ? w : w < wk.n_s + wk.n_w ? wk.w0 + (w - wk.n_s) : -1; };
+    auto page_of = [&](int u) {
+        int page = u >= 0 ? pt[u] : 0;
+        if ((unsigned)page >= (unsigned)n_pages) {
+            bad = true;
+            page = 0;
+        }
+        return page;
+    };
+    auto all_see = [&](int u) {
+        return u >= 0 && 16 * u + 16 <= wk.hi_min && (16 * u >= wk.lo_max || 16 * u + 16 <= wk.sk_min);
+    };
+    auto cache_bits = [&](int u) {
+        return u < 0 ? 0u : bits16(rs.lo - 16 * u, rs.hi - 16 * u) | bits16(-16 * u, rs.sk - 16 * u);
+    };
+    auto mask_bits = [&](int u) {
+        return u < 0 ? 0u : bits16(rs.ml - 16 * u, rs.m1 - 16 * u) | bits16(rs.m0 - 16 * u, rs.ms - 16 * u);
+    };
+
+    // softmax of one iteration's scores (two tiles of 16 keys; key of register e of tile t: bit key_bit(t, e))
+    auto key_bit = [&](int t, int e) { return QUADS ? 16 * t + 4 * kg + e : 8 * kg + 4 * t + e; };
+    auto softmax = [&](auto masked_c, f32x4 (&s)[2], unsigned vis, float (&p)[8]) __attribute__((always_inline)) {
+        constexpr bool MASKED = decltype(masked_c)::value;
+        float mx = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                if (MASKED) s[t][e] = ((vis >> key_bit(t, e)) & 1u) ? s[t][e] : -INFINITY;
+                mx = fmaxf(mx, s[t][e]);
+            }
+        if (__any(!(mx * scale <= m_run + kLag))) {      // rare: a row's first keys, or scores that outgrow the reference
+            mx = fmaxf(mx, __shfl_xor(mx, 16));
+            mx = fmaxf(mx, __shfl_xor(mx, 32));
+            if (!(mx * scale <= m_run + kLag)) {
+                const float m_new = fmaxf(m_run, ceilf(mx * scale));
+                const float alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+                l_run *= alpha;
+#pragma unroll
+                for (int t = 0; t < HT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[t][e] *= alpha;
+                m_run = m_new;
+            }
+        }
+        const float m_safe = m_run == -INFINITY ? 0.f : m_run;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) p[4 * t + e] = __builtin_amdgcn_exp2f(fmaf(s[t][e], scale, -m_safe));
+    };
+
+    if constexpr (BF) {
+        // ---- bf16: 16x16x32 MFMAs
+        auto body = [&](auto masked_c, const bf16x8 (&kf)[2][4], bf16x8 (&vf)[HT], unsigned vis) __attribute__((always_inline)) {
+            constexpr bool MASKED = decltype(masked_c)::value;
+            f32x4 s[2];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                s[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int j = 0; j < 4; ++j) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[t][j], qb[j], s[t], 0, 0, 0);
+            }
+            float p[8];
+            softmax(masked_c, s, vis, p);
+            const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
+            bf16x8 pf;
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                const bf16x2 pk = {(bf16_t)p[e], (bf16_t)p[e + 1]};
+                l_run = __builtin_amdgcn_fdot2_f32_bf16(pk, ones, l_run, false);
+                pf[e] = pk[0];
+                pf[e + 1] = pk[1];
+            }
+            if (MASKED) {
+                unsigned odd = 0;
+#pragma unroll
+                for (int t = 0; t < HT; ++t) {
+                    const u32x4 w = __builtin_bit_cast(u32x4, vf[t]);
+                    odd |= nonfinite2(w[0]) | nonfinite2(w[1]) | nonfinite2(w[2]) | nonfinite2(w[3]);
+                }
+                if (__builtin_expect(__any(odd != 0), 0)) {
+                    // V without them, and for every (value, row) how many of each kind its visible keys hold
+                    bf16x8 seen;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) seen[e] = (bf16_t)(float)((vis >> key_bit(e >> 2, e & 3)) & 1u);
+#pragma unroll
+                    for (int t = 0; t < HT; ++t) {
+                        bf16x8 pos, neg, nan, clean;
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float x = (float)vf[t][e];
+                            pos[e] = (bf16_t)(x == INFINITY ? 1.f : 0.f);
+                            neg[e] = (bf16_t)(x == -INFINITY ? 1.f : 0.f);
+                            nan[e] = (bf16_t)(x != x ? 1.f : 0.f);
+                            clean[e] = fabsf(x) < INFINITY ? vf[t][e] : (bf16_t)0.f;
+                        }
+                        const f32x4 z = {0.f, 0.f, 0.f, 0.f};
+                        const f32x4 n_pos = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pos, seen, z, 0, 0, 0);
+                        const f32x4 n_neg = __builtin_amdgcn_mfma_f32_16x16x32_bf16(neg, seen, z, 0, 0, 0);
+                        const f32x4 n_nan = __builtin_amdgcn_mfma_f32_16x16x32_bf16(nan, seen, z, 0, 0, 0);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            if (n_pos[e] > 0.f) acc[t][e] += INFINITY;
+                            if (n_neg[e] > 0.f) acc[t][e] -= INFINITY;
+                            if (n_nan[e] > 0.f) acc[t][e] = __builtin_nanf("");
+                        }
+                        vf[t] = clean;
+                    }
+                }
+            }
+#pragma unroll
+            for (int t = 0; t < HT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[t], pf, acc[t], 0, 0, 0);
+        };
+        const std::true_type masked;
+        const std::false_type plain;
+
+        // exact tiles, K [16][128] and V [128][16]: of a page or of the mask rows
+        auto load_exact = [&](const bf16_t *k0, const bf16_t *k1, const bf16_t *v0, const bf16_t *v1, bf16x8 (&kf)[2][4],
+                              bf16x8 (&vf)[HT]) __attribute__((always_inline)) {
+            if constexpr (KV4) {                         // two quads, blocks of 32 head-dim values to a quarter
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    kf[0][j] = *(const bf16x8 *)(k0 + lq * HD + 32 * kg + 8 * j);
+                    kf[1][j] = *(const bf16x8 *)(k1 + lq * HD + 32 * kg + 8 * j);
+                }
+#pragma unroll
+                for (int t = 0; t < HT; ++t) {
+                    const u32x2 x = *(const u32x2 *)(v0 + (HT * lq + t) * 16 + 4 * kg);
+                    const u32x2 y = *(const u32x2 *)(v1 + (HT * lq + t) * 16 + 4 * kg);
+                    vf[t] = __builtin_bit_cast(bf16x8, (u32x4){x[0], x[1], y[0], y[1]});
+                }
+            } else {                                     // eight keys in a row: tile t, row 4a + e is key 8a + 4t + e of the 32
+                const bf16_t *kb = (lq >> 3) ? k1 : k0, *vb = (kg >> 1) ? v1 : v0;
+#pragma unroll
+                for (int t = 0; t < 2; ++t)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        kf[t][j] = *(const bf16x8 *)(kb + (8 * ((lq >> 2) & 1) + 4 * t + (lq & 3)) * HD + 32 * j + 8 * kg);
+#pragma unroll
+                for (int t = 0; t < HT; ++t) vf[t] = *(const bf16x8 *)(vb + (16 * t + lq) * 16 + 8 * (kg & 1));
+            }
+        };
+        auto mask_tile = [&](int u) { return ((((size_t)b * n_kv + g) * n_mt + max(u, 0)) * 16) * HD; };
+        int n = it0 + wave;
+        for (; n < min(it1, wk.n1); n += 4) {
+            const int u0 = cache_unit(2 * n), u1 = cache_unit(2 * n + 1);
+            bf16x8 kf[2][4], vf[HT];
+            if constexpr (KV4) {
+                const unsigned char *p0 = c.kv4.pages + kv4_offset(c.kv4, page_of(u0), g);
+                const unsigned char *p1 = c.kv4.pages + kv4_offset(c.kv4, page_of(u1), g);
+                u32x4 kw[2], vw[2];
+                unsigned ks[2], vs[2];
+                const unsigned char *pp[2] = {p0, p1};
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    kw[t] = *(const u32x4 *)(pp[t] + kg * 256 + lq * 16);
+                    vw[t] = *(const u32x4 *)(pp[t] + kv4_v_codes(4) + kg * 256 + lq * 16);
+                    ks[t] = pp[t][kv4_k_scales(4) + kg * 16 + lq];
+                    vs[t] = *(const unsigned *)(pp[t] + kv4_v_scales(4) + (lq >> 2) * 16 + 4 * kg);
+                }
+#pragma unroll
+                for (int t = 0; t < 2; ++t) {
+                    const float s = kv4_scale(ks[t]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const bf16x2 x0 = kv4_pair_bf16<0>(kw[t][j], s), x1 = kv4_pair_bf16<1>(kw[t][j], s),
+                                     x2 = kv4_pair_bf16<2>(kw[t][j], s), x3 = kv4_pair_bf16<3>(kw[t][j], s);
+                        kf[t][j] = (bf16x8){x0[0], x0[1], x1[0], x1[1], x2[0], x2[1], x3[0], x3[1]};
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {        // token 4 kg + e: eight head-dim values of lane lq
+                        const float sv = kv4_scale((vs[t] >> (8 * e)) & 255u);
+                        const bf16x2 x0 = kv4_pair_bf16<0>(vw[t][e], sv), x1 = kv4_pair_bf16<1>(vw[t][e], sv),
+                                     x2 = kv4_pair_bf16<2>(vw[t][e], sv), x3 = kv4_pair_bf16<3>(vw[t][e], sv);
+                        const int at = 4 * t + e;
+                        vf[0][at] = x0[0]; vf[1][at] = x0[1]; vf[2][at] = x1[0]; vf[3][at] = x1[1];
+                        vf[4][at] = x2[0]; vf[5][at] = x2[1]; vf[6][at] = x3[0]; vf[7][at] = x3[1];
+                    }
+                }
+            } else {
+                const size_t o0 = ((size_t)page_of(u0) * n_kv + g) * 16 * HD, o1 = ((size_t)page_of(u1) * n_kv + g) * 16 * HD;
+                load_exact((const bf16_t *)c.kv.k_pages + o0, (const bf16_t *)c.kv.k_pages + o1,
+                           (const bf16_t *)c.kv.v_pages + o0, (const bf16_t *)c.kv.v_pages + o1, kf, vf);
+            }
+            if (all_see(u0) && all_see(u1)) body(plain, kf, vf, ~0u);
+            else body(masked, kf, vf, cache_bits(u0) | (cache_bits(u1) << 16));
+        }
+        for (; n < it1; n += 4) {
+            const int w = 2 * (n - wk.n1), u0 = wk.um0 + w, u1 = w + 1 < wk.n_m ? u0 + 1 : -1;
+            bf16x8 kf[2][4], vf[HT];
+            load_exact((const bf16_t *)c.k_scr + mask_tile(u0), (const bf16_t *)c.k_scr + mask_tile(u1),
+                       (const bf16_t *)c.v_scr + mask_tile(u0), (const bf16_t *)c.v_scr + mask_tile(u1), kf, vf);
+            body(masked, kf, vf, mask_bits(u0) | (mask_bits(u1) << 16));
+        }
+    } else {
+        // ---- fp32: 16x16x4 MFMAs.  A lane's head-dim values of O^T tile t are HT i + t.
+        const bool vec = hd % 4 == 0;
+        auto load_k = [&](const float *kp, float (&k)[Q4]) __attribute__((always_inline)) {      // token lq of a tile [16][hd]
+            const float *src = kp + lq * hd + Q4 * kg;
+            const int n = hd - Q4 * kg;
+#pragma unroll
+            for (int j = 0; j < Q4; j += 4) {
+                f32x4 x = {0.f, 0.f, 0.f, 0.f};
+                if (vec) {
+                    if (j < n) x = *(const f32x4 *)(src + j);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[e] = j + e < n ? src[j + e] : 0.f;
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) k[j + e] = x[e];
+            }
+        };
+        auto load_v = [&](const float *vp, f32x4 (&v)[HT]) __attribute__((always_inline)) {      // tokens 4 kg .. of [hd][16]
+#pragma unroll
+            for (int t = 0; t < HT; ++t) {
+                v[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+                if (HT * lq + t < hd) v[t] = *(const f32x4 *)(vp + (HT * lq + t) * 16 + 4 * kg);
+            }
+        };
+        auto load_k4 = [&](const unsigned char *blk, float (&k)[Q4]) __attribute__((always_inline)) {
+            const int nb = kv4_blocks(hd);
+#pragma unroll
+            for (int j = 0; j < Q4; j += 4) {
+                const int e0 = Q4 * kg + j, bl = e0 >> 5;
+                kv4_f32x2 x = {0.f, 0.f}, y = {0.f, 0.f};
+                if (e0 < hd) {
+                    const unsigned w = *(const unsigned short *)(blk + bl * 256 + lq * 16 + ((e0 & 31) >> 1));
+                    const float s = kv4_scale(blk[kv4_k_scales(nb) + bl * 16 + lq]);
+                    x = kv4_pair_f32<0>(w, s);
+                    y = kv4_pair_f32<1>(w, s);
+                }
+                k[j] = x[0]; k[j + 1] = x[1]; k[j + 2] = y[0]; k[j + 3] = y[1];
+            }
+        };
+        auto load_v4 = [&](const unsigned char *blk, f32x4 (&v)[HT]) __attribute__((always_inline)) {
+            const int nb = kv4_blocks(hd), e0 = HT * lq;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                unsigned w = 0;
+                float s = 0.f;
+                if (e0 < hd) {
+                    const unsigned char *src = blk + kv4_v_codes(nb) + (kg * 4 * nb + (e0 >> 3)) * 16 + e * 4 + ((e0 & 7) >> 1);
+                    if constexpr (HT == 8) w = *(const unsigned *)src;
+                    else if constexpr (HT == 4) w = *(const unsigned short *)src;
+                    else w = *src;
+                    s = kv4_scale(blk[kv4_v_scales(nb) + (e0 >> 5) * 16 + 4 * kg + e]);
+                }
+                const kv4_f32x2 x0 = kv4_pair_f32<0>(w, s), x1 = kv4_pair_f32<1>(w, s), x2 = kv4_pair_f32<2>(w, s),
+                                x3 = kv4_pair_f32<3>(w, s);
+                const float x[8] = {x0[0], x0[1], x1[0], x1[1], x2[0], x2[1], x3[0], x3[1]};
+#pragma unroll
+                for (int t = 0; t < HT; ++t) v[t][e] = x[t];
+            }
+        };
+        // the unit at hand: its scores, and what its weights add to the output
+        auto scores = [&](const float (&k)[Q4]) __attribute__((always_inline)) {
+            f32x4 s = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < Q4; ++j) s = __builtin_amdgcn_mfma_f32_16x16x4f32(k[j], qf[j], s, 0, 0, 0);
+            return s;
+        };
+        auto weigh = [&](f32x4 (&v)[HT], const float *p, unsigned vis16) __attribute__((always_inline)) {
+            unsigned top = 0;
+#pragma unroll
+            for (int t = 0; t < HT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) top = max(top, __float_as_uint(v[t][e]) & 0x7fffffffu);
+            if (__builtin_expect(__any(top >= 0x7f800000u), 0)) {
+#pragma unroll
+                for (int t = 0; t < HT; ++t) {
+                    f32x4 n_pos = {0.f, 0.f, 0.f, 0.f}, n_neg = n_pos, n_nan = n_pos;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float x = v[t][e], seen = (float)((vis16 >> (4 * kg + e)) & 1u);
+                        n_pos = __builtin_amdgcn_mfma_f32_16x16x4f32(x == INFINITY ? 1.f : 0.f, seen, n_pos, 0, 0, 0);
+                        n_neg = __builtin_amdgcn_mfma_f32_16x16x4f32(x == -INFINITY ? 1.f : 0.f, seen, n_neg, 0, 0, 0);
+                        n_nan = __builtin_amdgcn_mfma_f32_16x16x4f32(x != x ? 1.f : 0.f, seen, n_nan, 0, 0, 0);
+                        v[t][e] = fabsf(x) < INFINITY ? x : 0.f;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (n_pos[e] > 0.f) acc[t][e] += INFINITY;
+                        if (n_neg[e] > 0.f) acc[t][e] -= INFINITY;
+                        if (n_nan[e] > 0.f) acc[t][e] = __builtin_nanf("");
+                    }
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int t = 0; t < HT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[t][e], p[e], acc[t], 0, 0, 0);
+        };
+        for (int n = it0 + wave; n < it1; n += 4) {
+            const bool cache = n < wk.n1;
+            const int w = cache ? 2 * n : 2 * (n - wk.n1);
+            const int u[2] = {cache ? cache_unit(w) : wk.um0 + w, cache ? cache_unit(w + 1) : w + 1 < wk.n_m ? wk.um0 + w + 1 : -1};
+            size_t at[2];
+            f32x4 s[2], v[HT];
+            float k[Q4], p[8];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                const size_t piece = cache ? (size_t)page_of(u[t]) * n_kv + g : ((size_t)b * n_kv + g) * n_mt + max(u[t], 0);
+                at[t] = piece * 16 * hd;
+                if (KV4 && cache) load_k4(c.kv4.pages + piece * kv4_head_bytes(hd), k);
+                else load_k((const float *)(cache ? c.kv.k_pages : c.k_scr) + at[t], k);
+                if (KV4 && cache) at[t] = piece * kv4_head_bytes(hd);
+                s[t] = scores(k);
+            }
+            const unsigned vis = cache ? cache_bits(u[0]) | (cache_bits(u[1]) << 16) : mask_bits(u[0]) | (mask_bits(u[1]) << 16);
+            softmax(std::true_type(), s, vis, p);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) l_run += p[e];
+#pragma unroll
+            for (int t = 0; t < 2; ++t) {
+                if (KV4 && cache) load_v4(c.kv4.pages + at[t], v);
+                else load_v((const float *)(cache ? c.kv.v_pages : c.v_scr) + at[t], v);
+                weigh(v, p + 4 * t, vis >> (16 * t));
+            }
+        }
+    }
+
+    // ---- fold the four waves
+    float l = l_run;
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (bad) {
+        l = __builtin_nanf("");
+        if (m_run == -INFINITY) m_run = 0.f;
+    }
+    if (kg == 0) {
+        m_lds[wave][lq] = m_run;
+        l_lds[wave][lq] = l;
+    }
+#pragma unroll
+    for (int t = 0; t < HT; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int i = 4 * kg + e;
+            red[wave][lq][(BF && !KV4) ? 16 * t + i : HT * i + t] = acc[t][e];
+        }
+    __syncthreads();
+    constexpr int PER = HD / 16;                         // values of a thread
+    const int oq = tid >> 4, od = (tid & 15) * PER, of = tile * 16 + oq;
+    if (of >= F) return;
+    float m = m_lds[0][oq];
+#pragma unroll
+    for (int w = 1; w < 4; ++w) m = fmaxf(m, m_lds[w][oq]);
+    float sum = 0.f, o[PER];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) o[e] = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        const float mw = m_lds[w][oq];
+        if (mw == -INFINITY) continue;                   // saw nothing
+        const float wgt = mw == m ? 1.f : __builtin_amdgcn_exp2f(mw - m);
+        sum += wgt * l_lds[w][oq];
+#pragma unroll
+        for (int e = 0; e < PER; ++e) o[e] += wgt * red[w][oq][od + e];
+    }
+    const int ohq = of / d.R, orow = b * d.R + of - ohq * d.R;
+    const size_t orh = (size_t)orow * c.n_q + g * a.group + ohq;
+    if (a.splits > 1) {
+        const size_t at = orh * a.splits + split;
+        for (int e = 0; e < PER; ++e)
+            if (od + e < hd) a.opart[at * hd + od + e] = o[e];
+        if ((tid & 15) == 0) {
+            a.mpart[at] = m;
+            a.lpart[at] = sum;
+        }
+        return;
+    }
+    T *out = (T *)c.out + orh * hd + od;
+    if constexpr (BF) {
+        bf16x8 v;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (bf16_t)(o[e] / sum);
+        *(bf16x8 *)out = v;
+    } else {
+#pragma unroll
+        for (int e = 0; e < PER; ++e)
+            if (od + e < hd) out[e] = o[e] / sum;
+    }
+}
+
+// out[row][head] = sum_s w_s O_s / sum_s w_s l_s, w_s = 2^(m_s - max m).  A wave per (row, head).
+template <class T>
+__global__ __launch_bounds__(64) void span_combine_kernel(const float *__restrict__ opart, const float *__restrict__ mpart,
+                                                          const float *__restrict__ lpart, int splits, int hd,
+                                                          T *__restrict__ out) {
+    const size_t at = (size_t)blockIdx.x * splits;
+    const int lane = threadIdx.x;
+    float m = -INFINITY;
+    for (int s = lane; s < splits; s += 64) m = fmaxf(m, mpart[at + s]);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
+    float l = 0.f, x = 0.f, y = 0.f;
+    for (int s = 0; s < splits; ++s) {
+        const float ms = mpart[at + s];
+        if (ms == -INFINITY) continue;
+        const float w = ms == m ? 1.f : __builtin_amdgcn_exp2f(ms - m);
+        l += w * lpart[at + s];
+        if (lane < hd) x += w * opart[(at + s) * hd + lane];
+        if (lane + 64 < hd) y += w * opart[(at + s) * hd + lane + 64];
+    }
+    if (lane < hd) out[(size_t)blockIdx.x * hd + lane] = (T)(x / l);
+    if (lane + 64 < hd) out[(size_t)blockIdx.x * hd + lane + 64] = (T)(y / l);
+}
+
+}  // namespace
+
+SpanPlan plan_span(int dtype, int B, int n_q, int n_kv, int hd, const RowDesc &d, int window, int sinks, int max_prefix) {
+    SpanPlan p;
+    p.tiles = (n_q / n_kv * d.R + 15) / 16;
+    const long long wgs = (long long)B * n_kv * p.tiles;
+    // keys of a row: the window and the sinks, or all
+    long long keys = (long long)max_prefix + d.nc;
+    if (window > 0 && (long long)window + sinks + d.R < keys) keys = (long long)window + sinks + d.R;
+    const int bound = wgs >= 512 ? 1 : (int)std::min<long long>(64, 1024 / wgs);
+    p.splits = (int)std::max<long long>(1, std::min<long long>(bound, keys / 256));
+    p.part_floats = bound == 1 ? 0 : (size_t)B * d.R * n_q * bound * (hd + 2);
+    return p;
+}
+
+void launch_span_attention(int dtype, const SpanCall &c, const SpanPlan &p, hipStream_t st) {
+    SpanArgs a;
+    a.c = c;
+    const bool four = c.kv.k_pages == nullptr;
+    const int n_kv = four ? c.kv4.n_kv : c.kv.n_kv, hd = four ? c.kv4.hd : c.kv.hd;
+    a.group = c.n_q / n_kv;
+    a.tiles = p.tiles;
+    a.splits = p.splits;
+    const size_t rows = (size_t)c.B * c.d.R * c.n_q * p.splits;
+    a.opart = c.part;
+    a.mpart = c.part + rows * hd;
+    a.lpart = a.mpart + rows;
+    const dim3 grid(c.B * n_kv * p.tiles, p.splits);
+    auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(a); };
+    if (dtype == TIDAR_BF16) {
+        if (four) go(span_attn_kernel<bf16_t, true, 8>);
+        else go(span_attn_kernel<bf16_t, false, 8>);
+    } else if (four) {
+        if (hd <= 32) go(span_attn_kernel<float, true, 2>);
+        else if (hd <= 64) go(span_attn_kernel<float, true, 4>);
+        else go(span_attn_kernel<float, true, 8>);
+    } else {
+        if (hd <= 32) go(span_attn_kernel<float, false, 2>);
+        else if (hd <= 64) go(span_attn_kernel<float, false, 4>);
+        else go(span_attn_kernel<float, false, 8>);
+    }
+}
+
+void launch_span_combine(int dtype, const SpanCall &c, const SpanPlan &p, hipStream_t st) {
+    if (p.splits == 1) return;
+    const int hd = c.kv.k_pages ? c.kv.hd : c.kv4.hd;
+    const int heads = c.B * c.d.R * c.n_q;
+    const size_t rows = (size_t)heads * p.splits;
+    const float *m = c.part + rows * hd;
+    if (dtype == TIDAR_BF16)
+        span_combine_kernel<<<heads, 64, 0, st>>>(c.part, m, m + rows, p.splits, hd, (bf16_t *)c.out);
+    else
+        span_combine_kernel<<<heads, 64, 0, st>>>(c.part, m, m + rows, p.splits, hd, (float *)c.out);
+}

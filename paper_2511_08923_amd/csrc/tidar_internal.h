@@ -191,10 +191,18 @@ struct ChooseArgs {
     int mix_stride;
 };
 
+// A layer's 4-bit pages; their format and its conversions: kv4_format.h.
+struct Kv4View {
+    unsigned char *pages;
+    const int32_t *page_table;
+    int pages_per_seq, n_pages;
+    int n_kv, hd;
+};
+
 // Profiling hooks (defined in tidar_lib.hip).
 enum KernelClass {
     KC_EMBED = 0, KC_RMSNORM, KC_GEMM, KC_ROPE_KV, KC_ATTN, KC_ATTN_COMBINE, KC_SWIGLU, KC_ARGMAX, KC_VERIFY,
-    KC_PACK, KC_PLACE_KV, KC_SCORE, KC_COUNT
+    KC_PACK, KC_PLACE_KV, KC_SCORE, KC_TABLES, KC_KV4, KC_COUNT
 };
 
 struct GemmPlan {
@@ -389,3 +397,39 @@ void launch_finish_prefill(const int32_t *y, const int32_t *tokens, int tok_stri
                            int add_len, int last, int vocab, KvView kv, int32_t *prefix_len, int32_t *first_drafts,
                            hipStream_t st);
 void launch_set_i32(int32_t *p, int n, int32_t v, hipStream_t st);
+
+// ---- operators around the cache (kernels_cache.hip)
+void launch_table_extend(int batch, const int32_t *prefix_len, const int32_t *n_new, const int32_t *held,
+                         const int32_t *free_pages, int n_free, int32_t *page_table, int pages_per_seq, int n_pages,
+                         int32_t *row_start, int32_t *slots, int slot_cap, int32_t *held_out, int32_t *granted,
+                         int32_t *n_taken, hipStream_t st);
+void launch_kv4_store(int dtype, const Kv4View &kv, const int32_t *slots, int n_rows, const void *k, const void *v,
+                      hipStream_t st);
+void launch_kv4_load(int dtype, const Kv4View &kv, const int32_t *slots, int n_rows, void *k, void *v, hipStream_t st);
+// K/V of an attention call's rows: causal rows (where `kv` has pages) into the exact cache, mask rows as tiles of 16 into
+// k_scr [b][kv head][tile][16][hd] and v_scr [b][kv head][tile][hd][16].  k_new, v_new: n_rows rows per sequence, the mask rows
+// from row mask_row0 on.
+void launch_span_place(int dtype, const void *k_new, const void *v_new, int n_rows, int mask_row0, const int32_t *prefix_len,
+                       const RowDesc &d, int B, KvView kv, void *k_scr, void *v_scr, hipStream_t st);
+
+// ---- attention over a span of the cache: sliding window and sinks, exact or 4-bit pages (kernels_span.hip)
+struct SpanCall {
+    const void *q;
+    void *out;
+    KvView kv;                 // exact pages, or k_pages == nullptr:
+    Kv4View kv4;
+    const void *k_scr, *v_scr; // the mask rows' tiles
+    const int32_t *prefix_len;
+    RowDesc d;
+    int B, n_q;
+    int window, sinks;         // window 0: none
+    float *part;               // partial results of the key splits
+};
+struct SpanPlan {
+    int tiles;                 // query tiles per kv head
+    int splits;                // of the keys
+    size_t part_floats;
+};
+SpanPlan plan_span(int dtype, int B, int n_q, int n_kv, int hd, const RowDesc &d, int window, int sinks, int max_prefix);
+void launch_span_attention(int dtype, const SpanCall &c, const SpanPlan &p, hipStream_t st);
+void launch_span_combine(int dtype, const SpanCall &c, const SpanPlan &p, hipStream_t st);

@@ -5,13 +5,14 @@
 #include <new>
 #include <vector>
 
+#include "kv4_format.h"
 #include "tidar_internal.h"
 
 namespace {
 
 const char *kClassNames[KC_COUNT] = {"embed_rows", "rmsnorm", "gemm", "rope_kv", "attention", "attention_combine",
                                      "swiglu", "argmax_rows", "verify", "pack_weight", "place_kv",
-                                     "score_rows"};
+                                     "score_rows", "table_extend", "kv4_rows"};
 
 struct ProfEvent {
     int cls;
@@ -603,6 +604,58 @@ int prefill_together(const tidar_ctx *ctx, const int32_t *prompt_len, int n, int
     return 1;
 }
 
+// ---- around the cache
+constexpr int32_t kMostPositions = 1 << 30;         // of a sequence, and slots of a pool are below 2^31
+bool pool_ok(int32_t pages_per_seq, int32_t n_pages) {
+    return pages_per_seq > 0 && pages_per_seq <= kMostPositions / 16 && n_pages > 0 && n_pages <= 1 << 27;
+}
+bool aligned16(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+Kv4View layer_view4(const tidar_config &c, const tidar_kv4_cache *kv, int layer) {
+    Kv4View v;
+    v.pages = (unsigned char *)kv->pages + (size_t)layer * kv->n_pages * c.n_kv_heads * kv4_head_bytes(c.head_dim);
+    v.page_table = kv->page_table;
+    v.pages_per_seq = kv->pages_per_seq;
+    v.n_pages = kv->n_pages;
+    v.n_kv = c.n_kv_heads;
+    v.hd = c.head_dim;
+    return v;
+}
+
+// The rows of one attention call; false where they are not valid or too many (row indexes of a call are 32 bits).
+bool span_rows(int batch, int32_t n_causal, int32_t n_blocks, int32_t block_len, int32_t cond0, const tidar_config &c,
+               RowDesc *d) {
+    if (n_causal < 1 || n_blocks < 0 || block_len < 1 || block_len > TIDAR_MAX_K || cond0 < 0) return false;
+    if (n_blocks > 0 && (int64_t)cond0 + n_blocks - 1 > n_causal) return false;
+    const int64_t rows = (int64_t)n_causal + (int64_t)n_blocks * block_len;
+    if (rows * batch * c.n_q_heads > (int64_t)1 << 26) return false;
+    d->nc = n_causal;
+    d->nb = n_blocks;
+    d->bl = block_len;
+    d->cond0 = cond0;
+    d->cstride = 1;
+    d->nm = n_blocks * block_len;
+    d->R = (int)rows;
+    d->seq_base = 0;
+    return true;
+}
+
+struct SpanLayout {
+    SpanPlan plan;
+    size_t k_scr, v_scr, part, total;
+};
+SpanLayout span_layout(const tidar_config &c, int batch, const RowDesc &d, int window, int sinks, int max_prefix) {
+    SpanLayout l;
+    l.plan = plan_span(c.dtype, batch, c.n_q_heads, c.n_kv_heads, c.head_dim, d, window, sinks, max_prefix);
+    const size_t scr = align_up((size_t)batch * c.n_kv_heads * ((d.nm + 15) / 16) * 16 * c.head_dim * esize(c.dtype));
+    l.k_scr = 0;
+    l.v_scr = scr;
+    l.part = 2 * scr;
+    l.total = l.part + align_up(l.plan.part_floats * 4);
+    if (l.total < 256) l.total = 256;
+    return l;
+}
+
 size_t score_header_bytes(const tidar_config &c) { return align_up((size_t)c.max_batch * 4); }
 
 }  // namespace
@@ -944,6 +997,146 @@ tidar_status tidar_hybrid_attention(tidar_ctx *ctx, const tidar_kv_cache *kv, in
                              kUniform, M, c.n_q_heads, (float *)out, 0, st);
     }
     return TIDAR_OK;
+}
+
+// ---- around the cache
+
+size_t tidar_kv4_page_bytes(const tidar_ctx *ctx) {
+    return ctx ? (size_t)ctx->cfg.n_kv_heads * kv4_head_bytes(ctx->cfg.head_dim) : 0;
+}
+
+tidar_status tidar_table_extend(tidar_ctx *ctx, int32_t batch, const int32_t *prefix_len, const int32_t *n_new,
+                                const int32_t *held, const int32_t *free_pages, int32_t n_free, int32_t *page_table,
+                                int32_t pages_per_seq, int32_t n_pages, int32_t *row_start, int32_t *slots,
+                                int32_t slot_cap, int32_t *held_out, int32_t *granted, int32_t *n_taken, void *stream) {
+    if (!ctx || !prefix_len || !n_new || !held || !page_table || !row_start || !held_out || !granted || !n_taken)
+        return TIDAR_EINVAL;
+    if (batch < 1 || batch > ctx->cfg.max_batch || n_free < 0 || (n_free > 0 && !free_pages) || slot_cap < 0 ||
+        (slot_cap > 0 && !slots))
+        return TIDAR_EINVAL;
+    if (!pool_ok(pages_per_seq, n_pages) || (held < held_out + batch && held_out < held + batch)) return TIDAR_EINVAL;
+    hipStream_t st = (hipStream_t)stream;
+    Prof p(ctx, KC_TABLES, st);
+    launch_table_extend(batch, prefix_len, n_new, held, free_pages, n_free, page_table, pages_per_seq, n_pages, row_start,
+                        slots, slot_cap, held_out, granted, n_taken, st);
+    return TIDAR_OK;
+}
+
+static tidar_status kv4_rows(tidar_ctx *ctx, const tidar_kv4_cache *kv, int32_t layer, int32_t n_rows, const int32_t *slots,
+                             const void *k, const void *v, Kv4View *view) {
+    if (!ctx || !kv || !kv->pages || !aligned16(kv->pages) || layer < 0 || layer >= ctx->cfg.n_layers || n_rows < 0)
+        return TIDAR_EINVAL;
+    if (!pool_ok(1, kv->n_pages) || (n_rows > 0 && (!slots || !k || !v))) return TIDAR_EINVAL;
+    *view = layer_view4(ctx->cfg, kv, layer);
+    return TIDAR_OK;
+}
+
+tidar_status tidar_kv4_store(tidar_ctx *ctx, const tidar_kv4_cache *kv, int32_t layer, int32_t n_rows, const int32_t *slots,
+                             const void *k, const void *v, void *stream) {
+    Kv4View view;
+    const tidar_status rc = kv4_rows(ctx, kv, layer, n_rows, slots, k, v, &view);
+    if (rc != TIDAR_OK || n_rows == 0) return rc;
+    Prof p(ctx, KC_KV4, (hipStream_t)stream);
+    launch_kv4_store(ctx->cfg.dtype, view, slots, n_rows, k, v, (hipStream_t)stream);
+    return TIDAR_OK;
+}
+
+tidar_status tidar_kv4_load(tidar_ctx *ctx, const tidar_kv4_cache *kv, int32_t layer, int32_t n_rows, const int32_t *slots,
+                            void *k, void *v, void *stream) {
+    Kv4View view;
+    const tidar_status rc = kv4_rows(ctx, kv, layer, n_rows, slots, k, v, &view);
+    if (rc != TIDAR_OK || n_rows == 0) return rc;
+    Prof p(ctx, KC_KV4, (hipStream_t)stream);
+    launch_kv4_load(ctx->cfg.dtype, view, slots, n_rows, k, v, (hipStream_t)stream);
+    return TIDAR_OK;
+}
+
+tidar_status tidar_attention_workspace_bytes(const tidar_ctx *ctx, int32_t batch, int32_t n_causal, int32_t n_blocks,
+                                             int32_t block_len, int32_t max_prefix_len, size_t *bytes) {
+    if (!ctx || !bytes || batch < 1 || batch > ctx->cfg.max_batch || max_prefix_len < 0) return TIDAR_EINVAL;
+    RowDesc d;
+    if (!span_rows(batch, n_causal, n_blocks, block_len, 0, ctx->cfg, &d)) return TIDAR_EINVAL;
+    size_t most = 0;
+    for (int b = 1; b <= batch; ++b) {          // fewer sequences can take more key splits
+        const SpanLayout l = span_layout(ctx->cfg, b, d, 0, 0, max_prefix_len);
+        most = l.total > most ? l.total : most;
+    }
+    *bytes = most;
+    return TIDAR_OK;
+}
+
+// What the two attentions have in common: the checks, the mask rows' tiles, the attention and the join of its key splits.
+static tidar_status span_attention(tidar_ctx *ctx, const tidar_kv_cache *kv, const tidar_kv4_cache *kv4, int32_t layer,
+                                   int32_t batch, const int32_t *prefix_len, const void *q, const void *k_new,
+                                   const void *v_new, int32_t n_causal, int32_t n_blocks, int32_t block_len, int32_t cond0,
+                                   int32_t window, int32_t sinks, void *out, int32_t max_prefix_len_hint, void *ws,
+                                   size_t ws_bytes, void *stream) {
+    if (!ctx || !prefix_len || !q || !out || !ws || !aligned16(q) || !aligned16(out) || !aligned16(ws)) return TIDAR_EINVAL;
+    const tidar_config &c = ctx->cfg;
+    if (layer < 0 || layer >= c.n_layers || batch < 1 || batch > c.max_batch || max_prefix_len_hint < 0 || sinks < 0 ||
+        window < 0)
+        return TIDAR_EINVAL;
+    RowDesc d;
+    if (!span_rows(batch, n_causal, n_blocks, block_len, cond0, c, &d)) return TIDAR_EINVAL;
+    const int32_t pps = kv ? kv->pages_per_seq : kv4->pages_per_seq;
+    if ((int64_t)max_prefix_len_hint + n_causal > (int64_t)pps * TIDAR_PAGE_SIZE) return TIDAR_ECAPACITY;
+    const SpanLayout l = span_layout(c, batch, d, window, sinks, max_prefix_len_hint);
+    if (l.total > ws_bytes) return TIDAR_ENOMEM;
+    hipStream_t st = (hipStream_t)stream;
+    char *wsb = (char *)ws;
+    const KvView none = {nullptr, nullptr, nullptr, 0, 0, c.n_kv_heads, c.head_dim};
+    SpanCall call = {};
+    call.q = q;
+    call.out = out;
+    call.kv = kv ? layer_view(c, kv, layer) : none;
+    if (kv4) call.kv4 = layer_view4(c, kv4, layer);
+    call.k_scr = wsb + l.k_scr;
+    call.v_scr = wsb + l.v_scr;
+    call.prefix_len = prefix_len;
+    call.d = d;
+    call.B = batch;
+    call.n_q = c.n_q_heads;
+    call.window = window < kMostPositions ? window : kMostPositions;
+    call.sinks = sinks < kMostPositions ? sinks : kMostPositions;
+    call.part = (float *)(wsb + l.part);
+    if (kv || d.nm > 0) {
+        Prof p(ctx, KC_PLACE_KV, st);
+        launch_span_place(c.dtype, k_new, v_new, kv ? d.R : d.nm, kv ? d.nc : 0, prefix_len, d, batch, call.kv, wsb + l.k_scr,
+                          wsb + l.v_scr, st);
+    }
+    {
+        Prof p(ctx, KC_ATTN, st);
+        launch_span_attention(c.dtype, call, l.plan, st);
+    }
+    if (l.plan.splits > 1) {
+        Prof p(ctx, KC_ATTN_COMBINE, st);
+        launch_span_combine(c.dtype, call, l.plan, st);
+    }
+    return TIDAR_OK;
+}
+
+tidar_status tidar_window_attention(tidar_ctx *ctx, const tidar_kv_cache *kv, int32_t layer, int32_t batch,
+                                    const int32_t *prefix_len, const void *q, const void *k_new, const void *v_new,
+                                    int32_t n_causal, int32_t n_blocks, int32_t block_len, int32_t cond0, int32_t window,
+                                    int32_t sinks, void *out, int32_t max_prefix_len_hint, void *ws, size_t ws_bytes,
+                                    void *stream) {
+    if (!ctx || !kv_ok(ctx->cfg, kv) || !pool_ok(kv->pages_per_seq, kv->n_pages) || !aligned16(kv->k_pages) ||
+        !aligned16(kv->v_pages) || !k_new || !v_new || window < 1)
+        return TIDAR_EINVAL;
+    return span_attention(ctx, kv, nullptr, layer, batch, prefix_len, q, k_new, v_new, n_causal, n_blocks, block_len, cond0,
+                          window, sinks, out, max_prefix_len_hint, ws, ws_bytes, stream);
+}
+
+tidar_status tidar_kv4_attention(tidar_ctx *ctx, const tidar_kv4_cache *kv, int32_t layer, int32_t batch,
+                                 const int32_t *prefix_len, const void *q, const void *k_mask, const void *v_mask,
+                                 int32_t n_causal, int32_t n_blocks, int32_t block_len, int32_t cond0, int32_t window,
+                                 int32_t sinks, void *out, int32_t max_prefix_len_hint, void *ws, size_t ws_bytes,
+                                 void *stream) {
+    if (!ctx || !kv || !kv->pages || !aligned16(kv->pages) || !kv->page_table || !pool_ok(kv->pages_per_seq, kv->n_pages))
+        return TIDAR_EINVAL;
+    if ((n_blocks > 0 && (!k_mask || !v_mask)) || (window == 0 && sinks != 0)) return TIDAR_EINVAL;
+    return span_attention(ctx, nullptr, kv, layer, batch, prefix_len, q, k_mask, v_mask, n_causal, n_blocks, block_len, cond0,
+                          window, sinks, out, max_prefix_len_hint, ws, ws_bytes, stream);
 }
 
 size_t tidar_gemm_workspace_bytes(int32_t dtype, int32_t M, int32_t N, int32_t K) {
