@@ -143,7 +143,8 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 
 def _stream() -> int:
-    return torch.cuda.current_stream().cuda_stream
+    # the handle alone: torch.cuda.current_stream() builds a Stream object around it, 2.9 us of a call's host time against 0.3
+    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
 
 
 class tidar_ctx(C.c_void_p):
@@ -267,30 +268,39 @@ def tidar_score(ctx, w: tidar_weights, kv: tidar_kv_cache, batch: int, tokens: t
 _DTYPE = {TIDAR_F32: torch.float32, TIDAR_BF16: torch.bfloat16}
 
 
-def _mem(name: str, t: torch.Tensor, dtype: Optional[torch.dtype], numel: int) -> int:
+def _refuse(name: str, t: torch.Tensor, dtype: Optional[torch.dtype], numel: int, dev: int) -> None:
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{name}: {t.dtype}, expected {dtype}")
-    if not t.is_cuda or t.get_device() != torch.cuda.current_device():
+    if t.get_device() != dev:
         raise ValueError(f"{name}: on {t.device}, expected the current GPU")
     if not t.is_contiguous():
         raise ValueError(f"{name}: not contiguous (strides {tuple(t.stride())})")
-    if t.numel() < numel:
-        raise ValueError(f"{name}: {t.numel()} elements, expected at least {numel}")
+    raise ValueError(f"{name}: {t.numel()} elements, expected at least {numel}")
+
+
+def _mem(name: str, t: torch.Tensor, dtype: Optional[torch.dtype], numel: int, dev: int) -> int:
+    if t.numel() < numel or t.get_device() != dev or not t.is_contiguous() or (t.dtype != dtype and dtype is not None):
+        _refuse(name, t, dtype, numel, dev)
     return t.data_ptr()
+
+
+def _device() -> int:
+    return torch.cuda.current_device() if torch.cuda.is_available() else 0      # (no GPU: every tensor is refused)
 
 
 def tidar_table_extend(ctx: tidar_ctx, batch: int, prefix_len: torch.Tensor, n_new: torch.Tensor, held: torch.Tensor,
                        free_pages: Optional[torch.Tensor], n_free: int, page_table: torch.Tensor, n_pages: int,
                        row_start: torch.Tensor, slots: torch.Tensor, held_out: torch.Tensor, granted: torch.Tensor,
                        n_taken: torch.Tensor) -> None:
-    i32, pps = torch.int32, page_table.shape[-1]
-    _check(_lib.tidar_table_extend(ctx, batch, _mem("prefix_len", prefix_len, i32, batch), _mem("n_new", n_new, i32, batch),
-                                   _mem("held", held, i32, batch),
-                                   None if free_pages is None else _mem("free_pages", free_pages, i32, n_free), n_free,
-                                   _mem("page_table", page_table, i32, batch * pps), pps, n_pages,
-                                   _mem("row_start", row_start, i32, batch + 1), _mem("slots", slots, i32, 0), slots.numel(),
-                                   _mem("held_out", held_out, i32, batch), _mem("granted", granted, i32, batch), _mem("n_taken", n_taken, i32, 1), _stream()),
-           "tidar_table_extend")
+    i32, pps, dev = torch.int32, page_table.shape[-1], _device()
+    _check(_lib.tidar_table_extend(ctx, batch, _mem("prefix_len", prefix_len, i32, batch, dev),
+                                   _mem("n_new", n_new, i32, batch, dev), _mem("held", held, i32, batch, dev),
+                                   None if free_pages is None else _mem("free_pages", free_pages, i32, n_free, dev), n_free,
+                                   _mem("page_table", page_table, i32, batch * pps, dev), pps, n_pages,
+                                   _mem("row_start", row_start, i32, batch + 1, dev), _mem("slots", slots, i32, 0, dev),
+                                   slots.numel(), _mem("held_out", held_out, i32, batch, dev),
+                                   _mem("granted", granted, i32, batch, dev), _mem("n_taken", n_taken, i32, 1, dev),
+                                   _stream()), "tidar_table_extend")
 
 
 def tidar_kv4_page_bytes(ctx: tidar_ctx) -> int:
@@ -298,10 +308,10 @@ def tidar_kv4_page_bytes(ctx: tidar_ctx) -> int:
 
 
 def _kv4_rows(fn, where: str, ctx: tidar_ctx, kv, layer: int, n_rows: int, slots, k, v) -> None:
-    c = ctx.cfg
+    c, dev = ctx.cfg, _device()
     dt, n = _DTYPE[c.dtype], n_rows * c.n_kv_heads * c.head_dim
-    _check(fn(ctx, C.byref(kv), layer, n_rows, _mem("slots", slots, torch.int32, n_rows), _mem("k", k, dt, n),
-              _mem("v", v, dt, n), _stream()), where)
+    _check(fn(ctx, C.byref(kv), layer, n_rows, _mem("slots", slots, torch.int32, n_rows, dev), _mem("k", k, dt, n, dev),
+              _mem("v", v, dt, n, dev), _stream()), where)
 
 
 def tidar_kv4_store(ctx: tidar_ctx, kv: tidar_kv4_cache, layer: int, n_rows: int, slots: torch.Tensor, k: torch.Tensor,
@@ -316,13 +326,14 @@ def tidar_kv4_load(ctx: tidar_ctx, kv: tidar_kv4_cache, layer: int, n_rows: int,
 
 def _span_attention(fn, where: str, ctx: tidar_ctx, kv, layer, batch, prefix_len, q, k_new, v_new, new_rows, n_causal,
                     n_blocks, block_len, cond0, window, sinks, out, hint, ws) -> None:
-    c = ctx.cfg
+    c, dev = ctx.cfg, _device()
     dt, n_q = _DTYPE[c.dtype], batch * (n_causal + n_blocks * block_len) * c.n_q_heads * c.head_dim
     n_kv = batch * new_rows * c.n_kv_heads * c.head_dim
-    _check(fn(ctx, C.byref(kv), layer, batch, _mem("prefix_len", prefix_len, torch.int32, batch), _mem("q", q, dt, n_q),
-              None if k_new is None else _mem("k", k_new, dt, n_kv), None if v_new is None else _mem("v", v_new, dt, n_kv),
-              n_causal, n_blocks, block_len, cond0, window, sinks, _mem("out", out, dt, n_q), hint, _mem("ws", ws, None, 0),
-              ws.numel() * ws.element_size(), _stream()), where)
+    _check(fn(ctx, C.byref(kv), layer, batch, _mem("prefix_len", prefix_len, torch.int32, batch, dev),
+              _mem("q", q, dt, n_q, dev), None if k_new is None else _mem("k", k_new, dt, n_kv, dev),
+              None if v_new is None else _mem("v", v_new, dt, n_kv, dev), n_causal, n_blocks, block_len, cond0, window, sinks,
+              _mem("out", out, dt, n_q, dev), hint, _mem("ws", ws, None, 0, dev), ws.numel() * ws.element_size(),
+              _stream()), where)
 
 
 def tidar_window_attention(ctx: tidar_ctx, kv: tidar_kv_cache, layer: int, batch: int, prefix_len: torch.Tensor,

@@ -556,28 +556,67 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
     }
 }
 
-// out[row][head] = sum_s w_s O_s / sum_s w_s l_s, w_s = 2^(m_s - max m).  A wave per (row, head).
-template <class T>
+// out[row][head] = sum_s w_s O_s / sum_s w_s l_s, w_s = 2^(m_s - max m).  A wave per (row, head), lane = (8 head-dim values, one of 4
+// split lanes); a lane asks for all of J splits at once (one after another, 31 splits cost 31 trips to memory: 16 us).
+template <class T, int J>
 __global__ __launch_bounds__(64) void span_combine_kernel(const float *__restrict__ opart, const float *__restrict__ mpart,
                                                           const float *__restrict__ lpart, int splits, int hd,
                                                           T *__restrict__ out) {
     const size_t at = (size_t)blockIdx.x * splits;
-    const int lane = threadIdx.x;
-    float m = -INFINITY;
-    for (int s = lane; s < splits; s += 64) m = fmaxf(m, mpart[at + s]);
+    const int lane = threadIdx.x, d0 = 8 * (lane & 15), sl = lane >> 4;
+    const bool whole = d0 + 8 <= hd && hd % 4 == 0;
+    float m_all = lane < splits ? mpart[at + lane] : -INFINITY;          // at most 64 splits
+    float num[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f}, den = 0.f;
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) m = fmaxf(m, __shfl_xor(m, o));
-    float l = 0.f, x = 0.f, y = 0.f;
-    for (int s = 0; s < splits; ++s) {
-        const float ms = mpart[at + s];
-        if (ms == -INFINITY) continue;
-        const float w = ms == m ? 1.f : __builtin_amdgcn_exp2f(ms - m);
-        l += w * lpart[at + s];
-        if (lane < hd) x += w * opart[(at + s) * hd + lane];
-        if (lane + 64 < hd) y += w * opart[(at + s) * hd + lane + 64];
+    for (int o = 1; o < 64; o <<= 1) m_all = fmaxf(m_all, __shfl_xor(m_all, o));
+    for (int s0 = sl; s0 < splits; s0 += 4 * J) {
+        float m[J], l[J], x[J][8];
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            const int s = min(s0 + 4 * j, splits - 1);
+            m[j] = mpart[at + s];
+            l[j] = lpart[at + s];
+            const float *src = opart + (at + s) * hd + d0;
+            if (whole) {
+                const f32x4 a = *(const f32x4 *)src, b = *(const f32x4 *)(src + 4);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[j][e] = a[e];
+                    x[j][4 + e] = b[e];
+                }
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[j][e] = d0 + e < hd ? src[e] : 0.f;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < J; ++j) {
+            if (s0 + 4 * j >= splits || m[j] == -INFINITY) continue;
+            const float w = m[j] == m_all ? 1.f : __builtin_amdgcn_exp2f(m[j] - m_all);
+            den += w * l[j];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) num[e] += w * x[j][e];
+        }
     }
-    if (lane < hd) out[(size_t)blockIdx.x * hd + lane] = (T)(x / l);
-    if (lane + 64 < hd) out[(size_t)blockIdx.x * hd + lane + 64] = (T)(y / l);
+    den += __shfl_xor(den, 16);
+    den += __shfl_xor(den, 32);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        num[e] += __shfl_xor(num[e], 16);
+        num[e] += __shfl_xor(num[e], 32);
+    }
+    if (sl != 0) return;
+    T *dst = out + (size_t)blockIdx.x * hd + d0;
+    if constexpr (sizeof(T) == 2) {
+        bf16x8 o;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = (bf16_t)(num[e] / den);
+        *(bf16x8 *)dst = o;
+    } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            if (d0 + e < hd) dst[e] = num[e] / den;
+    }
 }
 
 }  // namespace
@@ -629,8 +668,11 @@ void launch_span_combine(int dtype, const SpanCall &c, const SpanPlan &p, hipStr
     const int heads = c.B * c.d.R * c.n_q;
     const size_t rows = (size_t)heads * p.splits;
     const float *m = c.part + rows * hd;
-    if (dtype == TIDAR_BF16)
-        span_combine_kernel<<<heads, 64, 0, st>>>(c.part, m, m + rows, p.splits, hd, (bf16_t *)c.out);
-    else
-        span_combine_kernel<<<heads, 64, 0, st>>>(c.part, m, m + rows, p.splits, hd, (float *)c.out);
+    auto go = [&](auto kernel, auto *out) { kernel<<<heads, 64, 0, st>>>(c.part, m, m + rows, p.splits, hd, out); };
+    if (dtype == TIDAR_BF16) {
+        if (p.splits <= 8) go(span_combine_kernel<bf16_t, 2>, (bf16_t *)c.out);
+        else go(span_combine_kernel<bf16_t, 8>, (bf16_t *)c.out);
+    } else {
+        go(span_combine_kernel<float, 4>, (float *)c.out);
+    }
 }
