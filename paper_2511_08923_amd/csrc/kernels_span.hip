@@ -21,98 +21,13 @@
 //
 // What a masked place holds never shows: scores are replaced by -inf, and infinities and NaN of V, which a weight of zero would
 // turn into NaN, are taken out of the product in units that are not wholly visible, and put back for the rows that see them.
+#include <stdlib.h>
 #include <algorithm>
 #include <type_traits>
 
-#include "kv4_format.h"
-#include "tidar_internal.h"
+#include "span_device.h"
 
 namespace {
-
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kLag = 16.f;                             // log2 of how far scores may outgrow the softmax reference
-typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
-typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-
-struct SpanArgs {
-    SpanCall c;
-    int group, tiles, splits;
-    float *opart, *mpart, *lpart;
-};
-
-// What one query row sees: cache keys [0, sk) and [lo, hi), mask rows [m0, ms) and [ml, m1).
-struct RowSpan {
-    int lo, hi, sk;
-    int m0, ms, ml, m1;
-};
-__device__ inline RowSpan row_span(const RowDesc &d, int r, int L, int window, int sinks) {
-    const RowInfo ri = row_info(d, r, L);
-    RowSpan s;
-    s.hi = L + ri.vis;
-    s.lo = window > 0 ? max(0, ri.pos - window + 1) : 0;
-    s.sk = window > 0 ? min(sinks, s.hi) : 0;
-    s.m0 = s.ms = s.ml = s.m1 = 0;
-    if (ri.blk >= 0) {                                   // mask row m of the block sits at position hi + m - m0
-        s.m0 = ri.blk * d.bl;
-        s.m1 = min(s.m0 + d.bl, d.nm);
-        s.ml = max(s.m0, s.m0 + s.lo - s.hi);
-        s.ms = window > 0 ? min(s.m1, s.m0 + sinks - s.hi) : s.m0;
-    }
-    return s;
-}
-__device__ inline unsigned bits16(int lo, int hi) {      // bits [lo, hi) of 16
-    lo = min(max(lo, 0), 16);
-    hi = min(max(hi, 0), 16);
-    return hi > lo ? ((1u << hi) - 1u) & ~((1u << lo) - 1u) : 0u;
-}
-
-// The units a tile of rows walks: cache units [0, n_s), [w0, w0 + n_w), then mask units [um0, um0 + n_m).
-struct Walk {
-    int n_s, w0, n_w, um0, n_m;
-    int n1, n2;                                          // iterations over the cache and over the mask tiles
-    int lo_max, hi_min, sk_min;                          // of the rows: a unit within all of their ranges needs no mask
-};
-__device__ inline Walk make_walk(const RowSpan &s, bool row, int window) {
-    // over the 16 rows (lanes of the same q hold the same row)
-    int lo0 = row ? s.lo : 0x7fffffff, lo1 = row ? s.lo : 0, hi0 = row ? s.hi : 0x7fffffff, hi1 = row ? s.hi : 0;
-    int sk0 = row ? s.sk : 0x7fffffff, sk1 = row ? s.sk : 0;
-    const bool mask = row && s.m1 > s.m0;
-    int m0 = mask ? s.m0 : 0x7fffffff, m1 = mask ? s.m1 : 0;
-#pragma unroll
-    for (int o = 1; o < 16; o <<= 1) {
-        lo0 = min(lo0, __shfl_xor(lo0, o));
-        lo1 = max(lo1, __shfl_xor(lo1, o));
-        hi0 = min(hi0, __shfl_xor(hi0, o));
-        hi1 = max(hi1, __shfl_xor(hi1, o));
-        sk0 = min(sk0, __shfl_xor(sk0, o));
-        sk1 = max(sk1, __shfl_xor(sk1, o));
-        m0 = min(m0, __shfl_xor(m0, o));
-        m1 = max(m1, __shfl_xor(m1, o));
-    }
-    Walk w;
-    auto uni = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
-    w.lo_max = uni(lo1);
-    w.hi_min = uni(hi0);
-    w.sk_min = uni(sk0);
-    w.n_s = uni(window > 0 ? (sk1 + 15) >> 4 : 0);
-    w.w0 = uni(lo0) >> 4;
-    const int w1 = (uni(hi1) + 15) >> 4;
-    if (w.n_s >= w.w0) {                                 // sinks and window meet
-        w.n_s = 0;
-        w.w0 = 0;
-    }
-    w.n_w = max(0, w1 - w.w0);
-    m0 = uni(m0);
-    m1 = uni(m1);
-    w.um0 = m1 > 0 ? m0 >> 4 : 0;
-    w.n_m = m1 > 0 ? ((m1 + 15) >> 4) - w.um0 : 0;
-    w.n1 = (w.n_s + w.n_w + 1) >> 1;
-    w.n2 = (w.n_m + 1) >> 1;
-    return w;
-}
-
-__device__ inline unsigned nonfinite2(unsigned x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
 
 // T: bf16 (head_dim 128) or float; KV4: 4-bit pages; HT: head_dim tiles of 16.
 template <class T, bool KV4, int HT>
@@ -139,7 +54,8 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
     const bool row = f < F;
     const int hq = row ? f / d.R : 0, r = row ? f - hq * d.R : 0;
     RowSpan rs = row_span(d, r, L, c.window, c.sinks);
-    const Walk wk = make_walk(rs, row, c.window);
+    const RowBounds rb = wave_bounds<16>(bounds_of(rs, row));
+    const Walk wk = walk_of(rb, c.window);
     if (!row) rs.hi = rs.lo = rs.sk = rs.m0 = rs.ms = rs.ml = rs.m1 = 0;
     const int n_it = fits ? wk.n1 + wk.n2 : 0, per = (n_it + a.splits - 1) / a.splits;
     const int it0 = min(n_it, split * per), it1 = min(n_it, it0 + per);
@@ -170,7 +86,7 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
     float m_run = -INFINITY, l_run = 0.f;
 
     // the unit (or -1) of walk position w
-    auto cache_unit = [&](int w) { return w < wk.n_s ? w : w < wk.n_s + wk.n_w ? wk.w0 + (w - wk.n_s) : -1; };
+    auto cache_unit = [&](int w) { return wk.cache_unit(w); };
     auto page_of = [&](int u) {
         int page = u >= 0 ? pt[u] : 0;
         if ((unsigned)page >= (unsigned)n_pages) {
@@ -179,16 +95,6 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
         }
         return page;
     };
-    auto all_see = [&](int u) {
-        return u >= 0 && 16 * u + 16 <= wk.hi_min && (16 * u >= wk.lo_max || 16 * u + 16 <= wk.sk_min);
-    };
-    auto cache_bits = [&](int u) {
-        return u < 0 ? 0u : bits16(rs.lo - 16 * u, rs.hi - 16 * u) | bits16(-16 * u, rs.sk - 16 * u);
-    };
-    auto mask_bits = [&](int u) {
-        return u < 0 ? 0u : bits16(rs.ml - 16 * u, rs.m1 - 16 * u) | bits16(rs.m0 - 16 * u, rs.ms - 16 * u);
-    };
-
     // softmax of one iteration's scores (two tiles of 16 keys; key of register e of tile t: bit key_bit(t, e))
     auto key_bit = [&](int t, int e) { return QUADS ? 16 * t + 4 * kg + e : 8 * kg + 4 * t + e; };
     auto softmax = [&](auto masked_c, f32x4 (&s)[2], unsigned vis, float (&p)[8]) __attribute__((always_inline)) {
@@ -355,15 +261,15 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
                 load_exact((const bf16_t *)c.kv.k_pages + o0, (const bf16_t *)c.kv.k_pages + o1,
                            (const bf16_t *)c.kv.v_pages + o0, (const bf16_t *)c.kv.v_pages + o1, kf, vf);
             }
-            if (all_see(u0) && all_see(u1)) body(plain, kf, vf, ~0u);
-            else body(masked, kf, vf, cache_bits(u0) | (cache_bits(u1) << 16));
+            if (all_see(rb, u0) && all_see(rb, u1)) body(plain, kf, vf, ~0u);
+            else body(masked, kf, vf, cache_bits(rs, u0) | (cache_bits(rs, u1) << 16));
         }
         for (; n < it1; n += 4) {
-            const int w = 2 * (n - wk.n1), u0 = wk.um0 + w, u1 = w + 1 < wk.n_m ? u0 + 1 : -1;
+            const int w = 2 * (n - wk.n1), u0 = wk.mask_unit(w), u1 = wk.mask_unit(w + 1);
             bf16x8 kf[2][4], vf[HT];
             load_exact((const bf16_t *)c.k_scr + mask_tile(u0), (const bf16_t *)c.k_scr + mask_tile(u1),
                        (const bf16_t *)c.v_scr + mask_tile(u0), (const bf16_t *)c.v_scr + mask_tile(u1), kf, vf);
-            body(masked, kf, vf, mask_bits(u0) | (mask_bits(u1) << 16));
+            body(masked, kf, vf, mask_bits(rs, u0) | (mask_bits(rs, u1) << 16));
         }
     } else {
         // ---- fp32: 16x16x4 MFMAs.  A lane's head-dim values of O^T tile t are HT i + t.
@@ -467,7 +373,7 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
         for (int n = it0 + wave; n < it1; n += 4) {
             const bool cache = n < wk.n1;
             const int w = cache ? 2 * n : 2 * (n - wk.n1);
-            const int u[2] = {cache ? cache_unit(w) : wk.um0 + w, cache ? cache_unit(w + 1) : w + 1 < wk.n_m ? wk.um0 + w + 1 : -1};
+            const int u[2] = {cache ? cache_unit(w) : wk.mask_unit(w), cache ? cache_unit(w + 1) : wk.mask_unit(w + 1)};
             size_t at[2];
             f32x4 s[2], v[HT];
             float k[Q4], p[8];
@@ -480,7 +386,7 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
                 if (KV4 && cache) at[t] = piece * kv4_head_bytes(hd);
                 s[t] = scores(k);
             }
-            const unsigned vis = cache ? cache_bits(u[0]) | (cache_bits(u[1]) << 16) : mask_bits(u[0]) | (mask_bits(u[1]) << 16);
+            const unsigned vis = cache ? cache_bits(rs, u[0]) | (cache_bits(rs, u[1]) << 16) : mask_bits(rs, u[0]) | (mask_bits(rs, u[1]) << 16);
             softmax(std::true_type(), s, vis, p);
 #pragma unroll
             for (int e = 0; e < 8; ++e) l_run += p[e];
@@ -621,9 +527,36 @@ __global__ __launch_bounds__(64) void span_combine_kernel(const float *__restric
 
 }  // namespace
 
+static int few_rows() {
+    const char *e = getenv("FEW_ROWS");
+    return e ? atoi(e) : 64;
+}
+#define kFewRows few_rows()
 SpanPlan plan_span(int dtype, int B, int n_q, int n_kv, int hd, const RowDesc &d, int window, int sinks, int max_prefix) {
     SpanPlan p;
-    p.tiles = (n_q / n_kv * d.R + 15) / 16;
+    const int F = n_q / n_kv * d.R;
+    p.rows = dtype == TIDAR_BF16 && F > kFewRows;
+    if (p.rows) {
+        p.tiles = (F + 127) / 128;
+        const long long base = (long long)B * n_kv * p.tiles;
+        const int bound = base >= 1024 ? 1 : (int)std::min<long long>(64, 2048 / base);
+        long long keys = (long long)max_prefix + d.R;
+        if (window > 0 && (long long)window + sinks + d.R < keys) keys = (long long)window + sinks + d.R;
+        const int iters = (int)((keys + 31) / 32), cap = std::min(bound, (iters + 3) / 4);
+        double best = 0.0;
+        p.splits = 1;
+        for (int s = 1; s <= cap; ++s) {
+            const double waves = (double)base * s / 512.0;
+            const double cost = (waves <= 1.0 ? 1.0 : d.nc >= 64 ? waves : waves + 0.5) * ((iters + s - 1) / s + 8);
+            if (s == 1 || cost < 0.97 * best) {
+                best = cost;
+                p.splits = s;
+            }
+        }
+        p.part_floats = bound == 1 ? 0 : (size_t)B * d.R * n_q * bound * (hd + 2);
+        return p;
+    }
+    p.tiles = (F + 15) / 16;
     const long long wgs = (long long)B * n_kv * p.tiles;
     // keys of a row: the window and the sinks, or all
     long long keys = (long long)max_prefix + d.nc;
@@ -646,6 +579,10 @@ void launch_span_attention(int dtype, const SpanCall &c, const SpanPlan &p, hipS
     a.opart = c.part;
     a.mpart = c.part + rows * hd;
     a.lpart = a.mpart + rows;
+    if (p.rows) {
+        launch_span_rows(a, p.tiles, st);
+        return;
+    }
     const dim3 grid(c.B * n_kv * p.tiles, p.splits);
     auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(a); };
     if (dtype == TIDAR_BF16) {

@@ -426,10 +426,17 @@ struct SpanCall {
     float *part;               // partial results of the key splits
 };
 struct SpanPlan {
-    int tiles;                 // query tiles per kv head
+    bool rows;                 // many rows (kernels_span_rows.hip): 128 to a workgroup, else 16
+    int tiles;                 // workgroups per kv head and key split
     int splits;                // of the keys
     size_t part_floats;
 };
+struct SpanArgs {
+    SpanCall c;
+    int group, tiles, splits;
+    float *opart, *mpart, *lpart;
+};
+void launch_span_rows(const SpanArgs &a, int chunks, hipStream_t st);
 SpanPlan plan_span(int dtype, int B, int n_q, int n_kv, int hd, const RowDesc &d, int window, int sinks, int max_prefix);
 void launch_span_attention(int dtype, const SpanCall &c, const SpanPlan &p, hipStream_t st);
 void launch_span_combine(int dtype, const SpanCall &c, const SpanPlan &p, hipStream_t st);
