@@ -317,8 +317,8 @@ __global__ __launch_bounds__(256) void kv4_load_kernel(RowArgs a, T *__restrict_
 // ------------------------------------------------------------------ new rows of an attention call
 // A workgroup takes the rows of one unit of 16 keys (a cache page of the causal rows, or a tile of mask rows) of one kv head:
 // V is turned to [hd][16] through LDS, so that a whole unit is written in runs of 16 tokens (row by row every 2-byte store
-// had a cache sector to itself).
-template <typename T>
+// had a cache sector to itself).  VEC: rows are read 16 bytes at a time.
+template <typename T, bool VEC>
 __global__ __launch_bounds__(256) void span_place_kernel(const T *__restrict__ k_new, const T *__restrict__ v_new, int n_rows,
                                                          int mask_row0, const int32_t *__restrict__ prefix_len, RowDesc d,
                                                          KvView kv, int n_cache_units, int units, T *__restrict__ k_scr,
@@ -350,15 +350,35 @@ __global__ __launch_bounds__(256) void span_place_kernel(const T *__restrict__ k
         vd = v_scr + tile;
     }
     const size_t src = (((size_t)b * n_rows + r0) * kv.n_kv + h) * hd, stride = (size_t)kv.n_kv * hd;
-    for (int i = tid; i < n * hd; i += 256) {
-        const int r = i / hd, e = i - r * hd;
-        kd[(s0 + r) * hd + e] = k_new[src + r * stride + e];
-        vt[s0 + r][e] = v_new[src + r * stride + e];
+    constexpr int E = 16 / sizeof(T);                     // elements of a 16-byte piece
+    typedef __attribute__((ext_vector_type(E))) T piece_t;
+    if (VEC) {
+        const int pieces = hd / E;
+        for (int i = tid; i < n * pieces; i += 256) {
+            const int r = i / pieces, e = (i - r * pieces) * E;
+            *(piece_t *)(kd + (s0 + r) * hd + e) = *(const piece_t *)(k_new + src + r * stride + e);
+            const piece_t x = *(const piece_t *)(v_new + src + r * stride + e);
+#pragma unroll
+            for (int j = 0; j < E; ++j) vt[s0 + r][e + j] = x[j];
+        }
+    } else {
+        for (int i = tid; i < n * hd; i += 256) {
+            const int r = i / hd, e = i - r * hd;
+            kd[(s0 + r) * hd + e] = k_new[src + r * stride + e];
+            vt[s0 + r][e] = v_new[src + r * stride + e];
+        }
     }
     __syncthreads();
-    for (int i = tid; i < 16 * hd; i += 256) {
-        const int e = i >> 4, s = i & 15;
-        if (s >= s0 && s < s0 + n) vd[i] = vt[s][e];
+    for (int i = tid; i < hd * (16 / E); i += 256) {      // a run of E tokens of one element
+        const int e = i / (16 / E), s = (i - e * (16 / E)) * E;
+        if (s >= s0 && s + E <= s0 + n) {
+            piece_t x;
+#pragma unroll
+            for (int j = 0; j < E; ++j) x[j] = vt[s + j][e];
+            *(piece_t *)(vd + e * 16 + s) = x;
+        } else {
+            for (int j = max(s, s0); j < min(s + E, s0 + n); ++j) vd[e * 16 + j] = vt[j][e];
+        }
     }
 }
 
@@ -369,12 +389,16 @@ void launch_span_place(int dtype, const void *k_new, const void *v_new, int n_ro
     const int cache_units = kv.k_pages ? (d.nc + 15) / 16 + 1 : 0, units = cache_units + (d.nm + 15) / 16;
     if (units == 0) return;
     const int grid = units * kv.n_kv * B;
-    if (dtype == TIDAR_BF16)
-        span_place_kernel<<<grid, 256, 0, st>>>((const bf16_t *)k_new, (const bf16_t *)v_new, n_rows, mask_row0, prefix_len, d,
-                                                kv, cache_units, units, (bf16_t *)k_scr, (bf16_t *)v_scr);
-    else
-        span_place_kernel<<<grid, 256, 0, st>>>((const float *)k_new, (const float *)v_new, n_rows, mask_row0, prefix_len, d,
-                                                kv, cache_units, units, (float *)k_scr, (float *)v_scr);
+    const bool vec = kv.hd % (dtype == TIDAR_BF16 ? 8 : 4) == 0 && (((uintptr_t)k_new | (uintptr_t)v_new) & 15) == 0;
+    auto go = [&](auto kernel, auto t) {
+        typedef decltype(t) T;
+        kernel<<<grid, 256, 0, st>>>((const T *)k_new, (const T *)v_new, n_rows, mask_row0, prefix_len, d, kv, cache_units, units,
+                                     (T *)k_scr, (T *)v_scr);
+    };
+    if (dtype == TIDAR_BF16 && vec) go(span_place_kernel<bf16_t, true>, bf16_t());
+    else if (dtype == TIDAR_BF16) go(span_place_kernel<bf16_t, false>, bf16_t());
+    else if (vec) go(span_place_kernel<float, true>, float());
+    else go(span_place_kernel<float, false>, float());
 }
 
 void launch_table_extend(int batch, const int32_t *prefix_len, const int32_t *n_new, const int32_t *held,

@@ -21,7 +21,6 @@
 //
 // What a masked place holds never shows: scores are replaced by -inf, and infinities and NaN of V, which a weight of zero would
 // turn into NaN, are taken out of the product in units that are not wholly visible, and put back for the rows that see them.
-#include <stdlib.h>
 #include <algorithm>
 #include <type_traits>
 
@@ -527,62 +526,55 @@ __global__ __launch_bounds__(64) void span_combine_kernel(const float *__restric
 
 }  // namespace
 
-static int few_rows() {
-    const char *e = getenv("FEW_ROWS");
-    return e ? atoi(e) : 64;
+constexpr int kFewRows = 64;           // rows of a kv head up to which they are taken 16 to a workgroup
+
+// Keys that a workgroup walks whose rows lie within `rows` positions, from the caller's bound on the prefix.
+long long span_keys(const RowDesc &d, int rows, int window, int sinks, int max_prefix) {
+    const long long all = (long long)max_prefix + d.R;
+    return window > 0 ? std::min(all, (long long)window + sinks + rows) : all;
 }
-#define kFewRows few_rows()
+
 SpanPlan plan_span(int dtype, int B, int n_q, int n_kv, int hd, const RowDesc &d, int window, int sinks, int max_prefix) {
-    SpanPlan p;
+    SpanPlan p = {};
     const int F = n_q / n_kv * d.R;
     p.rows = dtype == TIDAR_BF16 && F > kFewRows;
     if (p.rows) {
-        p.tiles = (F + 127) / 128;
-        const long long base = (long long)B * n_kv * p.tiles;
-        const int bound = base >= 1024 ? 1 : (int)std::min<long long>(64, 2048 / base);
-        long long keys = (long long)max_prefix + d.R;
-        if (window > 0 && (long long)window + sinks + d.R < keys) keys = (long long)window + sinks + d.R;
-        const int iters = (int)((keys + 31) / 32), cap = std::min(bound, (iters + 3) / 4);
-        double best = 0.0;
-        p.splits = 1;
-        for (int s = 1; s <= cap; ++s) {
-            const double waves = (double)base * s / 512.0;
-            const double cost = (waves <= 1.0 ? 1.0 : d.nc >= 64 ? waves : waves + 0.5) * ((iters + s - 1) / s + 8);
-            if (s == 1 || cost < 0.97 * best) {
-                best = cost;
-                p.splits = s;
-            }
-        }
-        p.part_floats = bound == 1 ? 0 : (size_t)B * d.R * n_q * bound * (hd + 2);
+        plan_span_rows(B, n_kv, n_q / n_kv, d, window, sinks, max_prefix, &p);
         return p;
     }
     p.tiles = (F + 15) / 16;
+    const long long keys = span_keys(d, d.R, window, sinks, max_prefix);
     const long long wgs = (long long)B * n_kv * p.tiles;
-    // keys of a row: the window and the sinks, or all
-    long long keys = (long long)max_prefix + d.nc;
-    if (window > 0 && (long long)window + sinks + d.R < keys) keys = (long long)window + sinks + d.R;
     const int bound = wgs >= 512 ? 1 : (int)std::min<long long>(64, 1024 / wgs);
     p.splits = (int)std::max<long long>(1, std::min<long long>(bound, keys / 256));
     p.part_floats = bound == 1 ? 0 : (size_t)B * d.R * n_q * bound * (hd + 2);
     return p;
 }
 
-void launch_span_attention(int dtype, const SpanCall &c, const SpanPlan &p, hipStream_t st) {
+static SpanArgs span_args(const SpanCall &c, const SpanPlan &p) {
     SpanArgs a;
     a.c = c;
-    const bool four = c.kv.k_pages == nullptr;
-    const int n_kv = four ? c.kv4.n_kv : c.kv.n_kv, hd = four ? c.kv4.hd : c.kv.hd;
+    const int n_kv = c.kv.k_pages ? c.kv.n_kv : c.kv4.n_kv, hd = c.kv.k_pages ? c.kv.hd : c.kv4.hd;
     a.group = c.n_q / n_kv;
     a.tiles = p.tiles;
     a.splits = p.splits;
-    const size_t rows = (size_t)c.B * c.d.R * c.n_q * p.splits;
+    a.span_rows = p.span_rows;
+    a.whole = p.whole;
+    const size_t rows = p.rows ? (size_t)(c.B * n_kv * p.tiles - p.whole) * p.splits * 128 : (size_t)c.B * c.d.R * c.n_q * p.splits;
     a.opart = c.part;
     a.mpart = c.part + rows * hd;
     a.lpart = a.mpart + rows;
+    return a;
+}
+
+void launch_span_attention(int dtype, const SpanCall &c, const SpanPlan &p, hipStream_t st) {
+    const SpanArgs a = span_args(c, p);
     if (p.rows) {
-        launch_span_rows(a, p.tiles, st);
+        launch_span_rows(a, st);
         return;
     }
+    const bool four = c.kv.k_pages == nullptr;
+    const int n_kv = four ? c.kv4.n_kv : c.kv.n_kv, hd = four ? c.kv4.hd : c.kv.hd;
     const dim3 grid(c.B * n_kv * p.tiles, p.splits);
     auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(a); };
     if (dtype == TIDAR_BF16) {
@@ -601,11 +593,14 @@ void launch_span_attention(int dtype, const SpanCall &c, const SpanPlan &p, hipS
 
 void launch_span_combine(int dtype, const SpanCall &c, const SpanPlan &p, hipStream_t st) {
     if (p.splits == 1) return;
+    const SpanArgs a = span_args(c, p);
+    if (p.rows) {
+        launch_span_rows_join(a, st);
+        return;
+    }
     const int hd = c.kv.k_pages ? c.kv.hd : c.kv4.hd;
     const int heads = c.B * c.d.R * c.n_q;
-    const size_t rows = (size_t)heads * p.splits;
-    const float *m = c.part + rows * hd;
-    auto go = [&](auto kernel, auto *out) { kernel<<<heads, 64, 0, st>>>(c.part, m, m + rows, p.splits, hd, out); };
+    auto go = [&](auto kernel, auto *out) { kernel<<<heads, 64, 0, st>>>(a.opart, a.mpart, a.lpart, p.splits, hd, out); };
     if (dtype == TIDAR_BF16) {
         if (p.splits <= 8) go(span_combine_kernel<bf16_t, 2>, (bf16_t *)c.out);
         else go(span_combine_kernel<bf16_t, 8>, (bf16_t *)c.out);

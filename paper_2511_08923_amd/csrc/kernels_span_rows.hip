@@ -1,19 +1,18 @@
-// The attention over a span for many query rows (bf16): the walk, the mask and the softmax of kernels_span.hip with tiles of 32
+// The attention over a span for many query rows (bf16): the walk, the mask and the softmax of kernels_span.hip with a tile of 32
 // query rows to a wave, four waves to a workgroup, and K and V tiles of 32 keys that the four share in LDS.
 //
 // Scores are v_mfma_f32_32x32x16_bf16 products S^T = K Q^T; a lane's registers 8u .. 8u + 7 are its row's scores of keys 8 lh ..
 // 8 lh + 7 of unit u, and after the exponential, packed, the B operand of O^T += V^T P^T.
 //
-// A wave works on two blocks at a time: the score products of block n + 1 stand between the vector instructions of block n's
-// softmax, and the output products of block n between the conversions (4-bit pages) or nothing (exact pages) of a tile three
-// blocks further on.  An MFMA takes 32 clocks and issues in 4; what stands between two of them is free up to eight vector
-// instructions, and with one block at a time a SIMD had either its matrix or its vector unit idle.
+// Tiles are staged in a ring of four.  Exact pages come by direct loads into LDS (lds_dma.h), three blocks ahead; of 4-bit
+// pages every thread converts 16 elements of K and 16 of V per tile, so a tile is converted once for 128 query rows.  K rows
+// of 256 bytes have their 16-byte pieces XOR-swizzled by the row and rows 4-7 and 8-11 of a unit exchanged; V^T is
+// [unit][key half][position] 16-byte pieces, where position p is head-dim value p (exact pages) or 8 (p % 16) + p / 16 (4-bit
+// pages: a wave's stores are contiguous then, and a lane's results are runs of eight values).
 //
-// Tiles are staged in a ring of four.  Exact pages come by direct loads into LDS (lds_dma.h); of 4-bit pages every thread
-// converts 16 elements of K and 16 of V per tile, so a tile is converted once for 128 query rows.  K rows of 256 bytes
-// have their 16-byte pieces XOR-swizzled by the row and rows 4-7 and 8-11 of a unit exchanged; V^T is [unit][key half][position]
-// 16-byte pieces, where position p is head-dim value p (exact pages) or 8 (p % 16) + p / 16 (4-bit pages: a wave's stores
-// are contiguous then, and a lane's results are runs of eight values).
+// Two workgroups share a compute unit, 512 run at a time.  As many whole ones as make full rounds go first; the walk of the rest,
+// whose round would leave most of the chip idle, is cut into key splits (SpanPlan), and only their partial results are written
+// and joined.
 #include <algorithm>
 #include <type_traits>
 
@@ -22,12 +21,70 @@
 
 namespace {
 
-constexpr int HD = 128, TILE = 32 * HD, RING = 4;
+constexpr int HD = 128, TILE = 32 * HD, RING = 4, ROWS = 128;
+
+// A workgroup's rows: which (sequence, kv head), and which of its rows.
+struct Place {
+    int b, g;
+    int f0, f1;                                          // rows [f0, f1) of the kv head's (head-major) list
+};
+__device__ inline Place place_of(const SpanArgs &a, int n_kv, int item) {
+    // The chunks of a (sequence, kv head) group run on one XCD where the groups divide evenly over the eight
+    // (workgroup i of a launch runs on XCD i % 8): its L2 then fetches the head's K and V once
+    const int n_groups = a.c.B * n_kv, F = a.group * a.c.d.R;
+    int grp, chunk;
+    if (n_groups % 8 == 0) {
+        const int j = item >> 3;
+        grp = (j / a.tiles) * 8 + (item & 7);
+        chunk = j % a.tiles;
+    } else {
+        grp = item / a.tiles;
+        chunk = item % a.tiles;
+    }
+    const int per_span = (a.span_rows + ROWS - 1) / ROWS, span = chunk / per_span;
+    Place p;
+    p.b = grp / n_kv;
+    p.g = grp - p.b * n_kv;
+    p.f0 = span * a.span_rows + (chunk - span * per_span) * ROWS;
+    p.f1 = min(min(p.f0 + ROWS, (span + 1) * a.span_rows), F);
+    return p;
+}
+
+// A lane's results: 16 pieces of four values (t, h) of its row, normalised, into the output.  KV4: value e of piece (t, h) is
+// head-dim value 8 (8 (h % 2) + 4 lh + e) + 2 t + h / 2; else 32 t + 8 h + 4 lh + e.
+template <bool KV4>
+__device__ inline void store_row(bf16_t *out, const f32x4 (&x)[4][4], float inv, int lh) {
+    if constexpr (KV4) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                bf16x8 o;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    o[2 * t] = (bf16_t)(x[t][h][e] * inv);
+                    o[2 * t + 1] = (bf16_t)(x[t][h + 2][e] * inv);
+                }
+                *(bf16x8 *)(out + 8 * (8 * h + 4 * lh + e)) = o;
+            }
+    } else {
+        typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int h = 0; h < 4; ++h)
+                *(bf16x4 *)(out + 32 * t + 8 * h + 4 * lh) = (bf16x4){(bf16_t)(x[t][h][0] * inv), (bf16_t)(x[t][h][1] * inv),
+                                                                      (bf16_t)(x[t][h][2] * inv), (bf16_t)(x[t][h][3] * inv)};
+    }
+}
+// Where the partial results of tile `wave` of a split are: 16 pieces as they lie in the registers, a store being one contiguous KiB.
+__device__ inline f32x4 *partial_of(const SpanArgs &a, int part, int wave) {
+    return (f32x4 *)a.opart + ((size_t)part * 4 + wave) * 16 * 64;
+}
 
 template <bool KV4>
 __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
-    constexpr int KRING = KV4 ? RING : RING + 1;         // direct loads of K are asked for an iteration earlier
-    __shared__ __attribute__((aligned(16))) bf16_t k_lds[KRING][TILE];
+    __shared__ __attribute__((aligned(16))) bf16_t k_lds[RING][TILE];
     __shared__ __attribute__((aligned(16))) bf16_t v_lds[RING][TILE];
     __shared__ RowBounds wave_rows[4];
     __shared__ int bad_lds;
@@ -37,26 +94,18 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
     const int lq = lane & 31, lh = lane >> 5;
     const int n_kv = KV4 ? c.kv4.n_kv : c.kv.n_kv;
     const int pps = KV4 ? c.kv4.pages_per_seq : c.kv.pages_per_seq, n_pages = KV4 ? c.kv4.n_pages : c.kv.n_pages;
-    // The chunks of a (sequence, kv head) group run on one XCD where the groups divide evenly over the eight
-    // (workgroup i of a launch runs on XCD i % 8): its L2 then fetches the head's K and V once
-    const int n_groups = c.B * n_kv, chunks = a.tiles;
-    int grp, chunk;
-    if (n_groups % 8 == 0) {
-        const int j = blockIdx.x >> 3;
-        grp = (j / chunks) * 8 + (blockIdx.x & 7);
-        chunk = j % chunks;
-    } else {
-        grp = blockIdx.x / chunks;
-        chunk = blockIdx.x % chunks;
-    }
-    const int split = blockIdx.y, b = grp / n_kv, g = grp - b * n_kv;
-    const int F = a.group * d.R;
+    const int cut = (int)blockIdx.x - a.whole, rest = c.B * n_kv * a.tiles - a.whole;          // cut >= 0: one of the key splits
+    const int splits = cut < 0 ? 1 : a.splits, split = cut < 0 ? 0 : cut / rest;
+    const int item = cut < 0 ? (int)blockIdx.x : a.whole + cut % rest;
+    const Place pl = place_of(a, n_kv, item);
+    const int b = pl.b, g = pl.g;
     const int L_raw = c.prefix_len[d.seq_base + b];
     const bool fits = L_raw >= 0 && (long long)L_raw + d.nc <= (long long)pps * 16;
     const int L = fits ? L_raw : 0;
-    const int tile = chunk * 4 + wave, f = tile * 32 + lq;
-    const bool here = tile * 32 < F, row = f < F;        // (here: wave-uniform)
+    const int f = pl.f0 + wave * 32 + lq;
+    const bool here = pl.f0 + wave * 32 < pl.f1, row = f < pl.f1;        // (here: wave-uniform)
     const int hq = row ? f / d.R : 0, r = row ? f - hq * d.R : 0;
+    const size_t orh = ((size_t)b * d.R + r) * c.n_q + g * a.group + hq;    // (row, head) in q and out
     RowSpan rs = row_span(d, r, L, c.window, c.sinks);
     const RowBounds rb = wave_bounds<32>(bounds_of(rs, row));
     if (!row) rs = RowSpan{};
@@ -67,22 +116,18 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
     auto uni = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
     const Walk wk = walk_of({uni(all.lo0), uni(all.lo1), uni(all.hi0), uni(all.hi1), uni(all.sk0), uni(all.sk1), uni(all.m0),
                              uni(all.m1)}, c.window);
-    const int n_it = fits ? wk.n1 + wk.n2 : 0, per = (n_it + a.splits - 1) / a.splits;
+    const int n_it = fits ? wk.n1 + wk.n2 : 0, per = (n_it + splits - 1) / splits;
     const int it0 = min(n_it, split * per), n_seq = min(n_it, it0 + per) - it0;
-    const __attribute__((address_space(4))) int32_t *pt = (const __attribute__((address_space(4))) int32_t *)(
-        (KV4 ? c.kv4.page_table : c.kv.page_table) + (size_t)(d.seq_base + b) * pps);
+    const int32_t *pt = (KV4 ? c.kv4.page_table : c.kv.page_table) + (size_t)(d.seq_base + b) * pps;
     const int n_mt = (d.nm + 15) >> 4;
     bool bad = !fits;
 
     // ---- Q: B operand, lane = (row, half of the 16 head-dim values of a step)
     bf16x8 qf[8];
-    {
-        const bf16_t *qp = (const bf16_t *)c.q + (((size_t)b * d.R + r) * c.n_q + (g * a.group + hq)) * HD + 8 * lh;
 #pragma unroll
-        for (int ks = 0; ks < 8; ++ks) {
-            qf[ks] = (bf16x8){0, 0, 0, 0, 0, 0, 0, 0};
-            if (row) qf[ks] = *(const bf16x8 *)(qp + 16 * ks);
-        }
+    for (int ks = 0; ks < 8; ++ks) {
+        qf[ks] = (bf16x8){0, 0, 0, 0, 0, 0, 0, 0};
+        if (row) qf[ks] = *(const bf16x8 *)((const bf16_t *)c.q + orh * HD + 8 * lh + 16 * ks);
     }
     const float scale = kLog2e / sqrtf((float)HD);
     f32x16 acc[4];
@@ -110,7 +155,6 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
     const int4v dvs = raw_desc((const bf16_t *)c.v_scr + scr0, (size_t)n_mt * 16 * HD * 2);
     const size_t layer_bytes = KV4 ? 0 : (size_t)c.kv.n_pages * n_kv * 16 * HD * 2;
     const int4v dk = raw_desc(c.kv.k_pages, layer_bytes), dv = raw_desc(c.kv.v_pages, layer_bytes);
-    auto k_slot = [&](int m) { return KV4 ? m & (RING - 1) : m % KRING; };
     auto dma_k = [&](int4v desc, int base, int slot) __attribute__((always_inline)) {
         const unsigned to = k_lds0 + slot * (TILE * 2) + (u_w * 16 + 8 * half_w) * 256;
 #pragma unroll
@@ -121,16 +165,22 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
 #pragma unroll
         for (int jj = 0; jj < 2; ++jj) dma16(to + 1024 * jj, v_voff[jj], desc, base);
     };
-    // The page of this wave's unit of tile m (0: it has none), asked for an iteration before it is needed.  All of this is scalar
-    // selects: with branches for the kinds of units an iteration took 2.5 times as long
-    const int n_cache = wk.n_s + wk.n_w, last_unit = max(0, wk.w0 + wk.n_w - 1);
-    auto page_at = [&](int m) {
-        const int w = 2 * (it0 + m) + u_w;
-        const bool in = m < n_seq && w < n_cache;
-        const int page = pt[min(w < wk.n_s ? w : wk.w0 + (w - wk.n_s), last_unit)];
-        return in ? page : 0;
+    // Page ids of this wave's units, 64 tiles at a time: lane i holds tile page0 + i's (0 for a unit that is not there), the
+    // next 64 are on their way.  (As scalar loads, one per iteration, they shared their counter with the LDS reads: every
+    // wait for LDS, the one in front of the barrier too, then waited for the table as well.)
+    const int n_cache = wk.n_s + wk.n_w;
+    auto load_pages = [&](int m0) {
+        const int m = m0 + lane, w = 2 * (it0 + m) + u_w;
+        return m < n_seq && w < n_cache ? pt[w < wk.n_s ? w : wk.w0 + (w - wk.n_s)] : 0;
     };
-    auto checked = [&](int page) {
+    int page0 = 0, pages = load_pages(0), pages_next = load_pages(64);
+    auto page_at = [&](int m) {
+        if (m - page0 >= 64) {
+            page0 += 64;
+            pages = pages_next;
+            pages_next = load_pages(page0 + 64);
+        }
+        const int page = __builtin_amdgcn_readlane(pages, m - page0);
         const bool in = (unsigned)page < (unsigned)n_pages;
         bad = bad || !in;
         return in ? page : 0;
@@ -152,7 +202,7 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
     const int k_src = kb * 256 + kt * 16 + kp * 8, ks_src = kv4_k_scales(4) + kb * 16 + kt;
     const int v_src = kv4_v_codes(4) + (vt >> 2) * 256 + vi * 16 + (vt & 3) * 4, vs_src = kv4_v_scales(4) + (vi >> 2) * 16 + vt;
     auto fetch = [&](int page) __attribute__((always_inline)) {
-        const unsigned char *p = c.kv4.pages + kv4_offset(c.kv4, checked(page), g);
+        const unsigned char *p = c.kv4.pages + kv4_offset(c.kv4, page, g);
         return Raw{*(const u32x2 *)(p + k_src), *(const u32x2 *)(p + v_src), p[ks_src], *(const unsigned short *)(p + vs_src)};
     };
     auto convert = [&](const Raw &x, int slot) __attribute__((always_inline)) {
@@ -186,27 +236,32 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
             wait_loads<0>();
         }
     };
-    // exact pages and mask rows: two direct loads of K or V of tile m; of a tile that there is not, through a buffer of no bytes
-    auto from = [&](int4v pages, int4v rows, int m) {
-        int4v desc;
+    // exact pages and mask rows: four direct loads of tile m; of a tile that there is not, through a buffer of no bytes
+    auto ask = [&](int m, int page) __attribute__((always_inline)) {
         const bool mask = it0 + m >= wk.n1;
+        int4v kd, vd;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) desc[i] = mask ? rows[i] : pages[i];
-        desc[2] = m < n_seq ? desc[2] : 0;
-        return desc;
-    };
-    auto ask_k = [&](int m, int page) __attribute__((always_inline)) {
-        dma_k(from(dk, dks, m), it0 + m >= wk.n1 ? mask_base(m) : page_base(page), k_slot(m));
-    };
-    auto ask_v = [&](int m, int page) __attribute__((always_inline)) {
-        dma_v(from(dv, dvs, m), it0 + m >= wk.n1 ? mask_base(m) : page_base(page), m & (RING - 1));
+        for (int i = 0; i < 4; ++i) {
+            kd[i] = mask ? dks[i] : dk[i];
+            vd[i] = mask ? dvs[i] : dv[i];
+        }
+        kd[2] = m < n_seq ? kd[2] : 0;
+        vd[2] = m < n_seq ? vd[2] : 0;
+        const int base = mask ? mask_base(m) : page_base(page);
+        dma_k(kd, base, m & (RING - 1));
+        dma_v(vd, base, m & (RING - 1));
     };
 
     // K as A operand: lane = (tile row, half of the step); V^T as A operand: lane = (position, key half of the unit)
-    auto k_frags = [&](int m, bf16x8 (&kf)[8]) __attribute__((always_inline)) {
-        const unsigned char *p = reinterpret_cast<const unsigned char *>(&k_lds[k_slot(m)][0]) + lq * 256;
+    auto scores = [&](int m, f32x16 &s) __attribute__((always_inline)) {
+        const unsigned char *p = reinterpret_cast<const unsigned char *>(&k_lds[m & (RING - 1)][0]) + lq * 256;
+        bf16x8 kf[8];
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) kf[ks] = *(const bf16x8 *)(p + (((2 * ks + lh) ^ (lq & 15)) << 4));
+#pragma unroll
+        for (int e = 0; e < 16; ++e) s[e] = 0.f;
+#pragma unroll
+        for (int ks = 0; ks < 8; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[ks], s, 0, 0, 0);
     };
     auto v_frags = [&](int m, bf16x8 (&vf)[4][2]) __attribute__((always_inline)) {
         const unsigned char *p = reinterpret_cast<const unsigned char *>(&v_lds[m & (RING - 1)][0]);
@@ -215,15 +270,9 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
 #pragma unroll
             for (int u = 0; u < 2; ++u) vf[t][u] = *(const bf16x8 *)(p + (((u * 2 + lh) * 128 + 32 * t + lq) << 4));
     };
-    auto scores = [&](const bf16x8 (&kf)[8], f32x16 &s) __attribute__((always_inline)) {
-#pragma unroll
-        for (int e = 0; e < 16; ++e) s[e] = 0.f;
-#pragma unroll
-        for (int ks = 0; ks < 8; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[ks], s, 0, 0, 0);
-    };
     // V^T values that are not finite, of a block that not every row sees whole: taken out of the fragments, and added for the
     // rows that see them, key by key from LDS (rare, and written to need few registers)
-    auto set_aside = [&](int m, bf16x8 (&vf)[4][2], unsigned vis32) __attribute__((always_inline)) {
+    auto set_aside = [&](int m, bf16x8 (&vf)[4][2], unsigned vis) __attribute__((always_inline)) {
         unsigned odd = 0;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -237,13 +286,13 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
 #pragma unroll 1
             for (int key = 0; key < 32; ++key) {
                 const unsigned short *p = v + (key >> 3) * 1024 + (key & 7) + 32 * lh;
-                const bool seen = (vis32 >> key) & 1u;
 #pragma unroll
                 for (int t = 0; t < 4; ++t)
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         const float x = __uint_as_float((unsigned)p[(32 * t + 8 * (e >> 2) + (e & 3)) * 8] << 16);
-                        acc[t][e] += seen && !(fabsf(x) < INFINITY) ? x : 0.f;
+                        const float y = fabsf(x) < INFINITY ? 0.f : x;
+                        acc[t][e] += ((vis >> key) & 1u) ? y : 0.f;
                     }
             }
 #pragma unroll
@@ -261,99 +310,50 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
         }
     };
 
-    Raw r0 = {}, r1 = {};
-    int page = 0, page_v = 0;                            // of the next tile to be asked for, and of the last one
+    // Tiles to come.  At the start of iteration n the codes of tile n + 5 (4-bit pages) or tile n + 3 itself (exact pages) are
+    // asked for; at its end tile n + 3 is converted, or tile n + 1 has landed.
+    Raw r0 = {}, r1 = {}, r2 = {};
     if constexpr (KV4) {
 #pragma unroll
         for (int m = 0; m < 3; ++m) stage4(m, fetch(page_at(m)));
         r0 = fetch(page_at(3));
         r1 = fetch(page_at(4));
-        page = page_at(5);
     } else {
 #pragma unroll
-        for (int m = 0; m < 4; ++m) {
-            page_v = checked(page_at(m));
-            ask_k(m, page_v);
-            if (m < 3) ask_v(m, page_v);
-        }
-        page = page_at(4);
+        for (int m = 0; m < 3; ++m) ask(m, page_at(m));
     }
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) asm volatile("" : "+v"(qf[ks]));      // no wait for Q inside the loop
     wait_loads<0>();
     lds_barrier();
-    f32x16 s;
-    bf16x8 kf[8];
-    if (here) {
-        k_frags(0, kf);
-        scores(kf, s);
-        k_frags(1, kf);
-    }
-    // the reference of a row, moved where the block's scores outgrow it (rare)
-    auto reference = [&]() __attribute__((always_inline)) {
-        float mx = -INFINITY;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[e]);
-        if (__builtin_expect(__any(!(mx * scale <= m_run + kLag)), 0)) {
-            mx = fmaxf(mx, __shfl_xor(mx, 32));
-            const bool grow = !(mx * scale <= m_run + kLag);
-            const float m_new = grow ? fmaxf(m_run, ceilf(mx * scale)) : m_run;
-            const float alpha = grow ? __builtin_amdgcn_exp2f(m_run - m_new) : 1.f;
-            l_run *= alpha;
-#pragma unroll
-            for (int t = 0; t < 4; ++t)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) acc[t][e] *= alpha;
-            m_run = m_new;
-        }
+    auto begin = [&](int n) __attribute__((always_inline)) {
+        if constexpr (KV4) r2 = fetch(page_at(n + 5));
+        else ask(n + 3, page_at(n + 3));
     };
-    // scores of the next block between the numerators of this one
-    auto numerators = [&](f32x16 &s_next, bf16x8 (&pf)[2]) __attribute__((always_inline)) {
-        scores(kf, s_next);
-        const float m_safe = m_run == -INFINITY ? 0.f : m_run;
-        const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
-#pragma unroll
-        for (int e = 0; e < 16; e += 2) {
-            const bf16x2 pk = {(bf16_t)__builtin_amdgcn_exp2f(fmaf(s[e], scale, -m_safe)),
-                               (bf16_t)__builtin_amdgcn_exp2f(fmaf(s[e + 1], scale, -m_safe))};
-            l_run = __builtin_amdgcn_fdot2_f32_bf16(pk, ones, l_run, false);
-            pf[e >> 3][e & 7] = pk[0];
-            pf[e >> 3][(e & 7) + 1] = pk[1];
-        }
-    };
-    auto outputs = [&](const bf16x8 (&vf)[4][2], const bf16x8 (&pf)[2]) __attribute__((always_inline)) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int t = 0; t < 4; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[t][u], pf[u], acc[t], 0, 0, 0);
-    };
-    // the tiles to come: 4-bit pages, the tile three blocks on; exact pages, K of block n + 4 and V of n + 3, which are needed
-    // two iterations on
-    auto ahead = [&](int n) __attribute__((always_inline)) {
+    auto finish = [&](int n) __attribute__((always_inline)) {
         if constexpr (KV4) {
             stage4(n + 3, r0);
             r0 = r1;
-            r1 = fetch(page);
-            page = page_at(n + 6);
+            r1 = r2;
         } else {
-            const int page_k = checked(page);
-            page = page_at(n + 5);
-            ask_k(n + 4, page_k);
-            ask_v(n + 3, page_v);
-            page_v = page_k;
-            wait_loads<4>();                             // what was asked for before has landed
+            wait_loads<8>();
         }
         lds_barrier_counted();
     };
     if (!here) {                                         // no rows: this wave only moves tiles
-        for (int n = 0; n < n_seq; ++n) ahead(n);
+        for (int n = 0; n < n_seq; ++n) {
+            begin(n);
+            finish(n);
+        }
     } else {
         // blocks [f0, f1) are cache units that every row of the wave sees whole: no predicate there
         const int base = wk.w0 - wk.n_s + 2 * it0;
         const int f0 = max(((wk.n_s + 1) >> 1) - it0, ((((rb.lo1 + 15) >> 4) - base) + 1) >> 1), f1 = ((rb.hi0 >> 4) - base) >> 1;
         for (int n = 0; n < n_seq; ++n) {
+            begin(n);
+            f32x16 s;
+            scores(n, s);
             bf16x8 vf[4][2], pf[2];
-            f32x16 s_next;
             v_frags(n, vf);
             unsigned vis = 0;
             const bool masked = n < f0 || n >= f1;
@@ -366,13 +366,38 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[e] = ((mine >> ((e & 7) + 16 * (e >> 3))) & 1u) ? s[e] : -INFINITY;
             }
-            reference();
+            // the reference of a row, moved where the block's scores outgrow it (rare)
+            float mx = -INFINITY;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[e]);
+            if (__builtin_expect(__any(!(mx * scale <= m_run + kLag)), 0)) {
+                mx = fmaxf(mx, __shfl_xor(mx, 32));
+                if (!(mx * scale <= m_run + kLag)) {
+                    const float m_new = fmaxf(m_run, ceilf(mx * scale)), alpha = __builtin_amdgcn_exp2f(m_run - m_new);
+                    l_run *= alpha;
+#pragma unroll
+                    for (int t = 0; t < 4; ++t)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) acc[t][e] *= alpha;
+                    m_run = m_new;
+                }
+            }
             if (masked) set_aside(n, vf, vis);           // (behind the rescale: a factor of zero would make NaN of infinity)
-            numerators(s_next, pf);
-            k_frags(n + 2, kf);
-            outputs(vf, pf);
-            s = s_next;
-            ahead(n);
+            const float m_safe = m_run == -INFINITY ? 0.f : m_run;
+            const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+                const bf16x2 pk = {(bf16_t)__builtin_amdgcn_exp2f(fmaf(s[e], scale, -m_safe)),
+                                   (bf16_t)__builtin_amdgcn_exp2f(fmaf(s[e + 1], scale, -m_safe))};
+                l_run = __builtin_amdgcn_fdot2_f32_bf16(pk, ones, l_run, false);
+                pf[e >> 3][e & 7] = pk[0];
+                pf[e >> 3][(e & 7) + 1] = pk[1];
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[t][u], pf[u], acc[t], 0, 0, 0);
+            finish(n);
         }
     }
 
@@ -386,58 +411,127 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
         l = __builtin_nanf("");
         if (m_run == -INFINITY) m_run = 0.f;
     }
-    if (!row) return;
-    const size_t orh = ((size_t)b * d.R + r) * c.n_q + g * a.group + hq;
-    const size_t at = orh * a.splits + split;
-    const float inv = 1.f / l;
-    if (a.splits > 1 && lh == 0) {
-        a.mpart[at] = m_run;
-        a.lpart[at] = l;
+    f32x4 x[4][4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int h = 0; h < 4; ++h) x[t][h] = (f32x4){acc[t][4 * h], acc[t][4 * h + 1], acc[t][4 * h + 2], acc[t][4 * h + 3]};
+    if (cut < 0) {
+        if (row) store_row<KV4>((bf16_t *)c.out + orh * HD, x, 1.f / l, lh);
+        return;
     }
-    if constexpr (KV4) {                                 // runs of eight: values 8 i .. + 7 of i = 8 h + 4 lh + e
+    const int part = (item - a.whole) * a.splits + split;
+    f32x4 *op = partial_of(a, part, wave) + lane;
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+    for (int t = 0; t < 4; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int d0 = 8 * (8 * h + 4 * lh + e);
-                float x[8];
-#pragma unroll
-                for (int t = 0; t < 4; ++t) {
-                    x[2 * t] = acc[t][4 * h + e];
-                    x[2 * t + 1] = acc[t][8 + 4 * h + e];
-                }
-                if (a.splits > 1) {
-                    *(f32x4 *)(a.opart + at * HD + d0) = (f32x4){x[0], x[1], x[2], x[3]};
-                    *(f32x4 *)(a.opart + at * HD + d0 + 4) = (f32x4){x[4], x[5], x[6], x[7]};
-                } else {
-                    bf16x8 o;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) o[i] = (bf16_t)(x[i] * inv);
-                    *(bf16x8 *)((bf16_t *)c.out + orh * HD + d0) = o;
-                }
-            }
-    } else {
-        typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
-#pragma unroll
-        for (int t = 0; t < 4; ++t)
-#pragma unroll
-            for (int h = 0; h < 4; ++h) {
-                const int d0 = 32 * t + 8 * h + 4 * lh;
-                const f32x4 x = {acc[t][4 * h], acc[t][4 * h + 1], acc[t][4 * h + 2], acc[t][4 * h + 3]};
-                if (a.splits > 1)
-                    *(f32x4 *)(a.opart + at * HD + d0) = x;
-                else
-                    *(bf16x4 *)((bf16_t *)c.out + orh * HD + d0) =
-                        (bf16x4){(bf16_t)(x[0] * inv), (bf16_t)(x[1] * inv), (bf16_t)(x[2] * inv), (bf16_t)(x[3] * inv)};
-            }
+        for (int h = 0; h < 4; ++h) op[(4 * t + h) * 64] = x[t][h];
+    if (lh == 0) {
+        a.mpart[(size_t)part * ROWS + wave * 32 + lq] = m_run;
+        a.lpart[(size_t)part * ROWS + wave * 32 + lq] = l;
     }
 }
 
+// out = sum_s w_s O_s / sum_s w_s l_s, w_s = 2^(m_s - max m), of the workgroups that were cut: a wave takes a quarter of the results
+// of a tile of 32 rows.
+template <bool KV4>
+__global__ __launch_bounds__(256) void span_rows_join_kernel(SpanArgs a) {
+    const SpanCall &c = a.c;
+    const RowDesc &d = c.d;
+    const int lane = threadIdx.x & 63, lq = lane & 31, lh = lane >> 5, t = threadIdx.x >> 6, wave = blockIdx.x & 3;
+    const int tail = blockIdx.x >> 2, n_kv = KV4 ? c.kv4.n_kv : c.kv.n_kv;
+    const Place pl = place_of(a, n_kv, a.whole + tail);
+    const int f = pl.f0 + wave * 32 + lq;
+    if (pl.f0 + wave * 32 >= pl.f1) return;
+    const int S = a.splits, part = tail * S;
+    const float *mp = a.mpart + (size_t)part * ROWS + wave * 32 + lq, *lp = a.lpart + (size_t)part * ROWS + wave * 32 + lq;
+    float m = -INFINITY;
+#pragma unroll 8
+    for (int s = 0; s < S; ++s) m = fmaxf(m, mp[(size_t)s * ROWS]);
+    f32x4 num[4];
+    float den = 0.f;
+#pragma unroll
+    for (int h = 0; h < 4; ++h) num[h] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < S; s0 += 4) {
+        f32x4 x[4][4];
+        float ms[4], ls[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int s = min(s0 + j, S - 1);
+            const f32x4 *op = partial_of(a, part + s, wave) + 4 * t * 64 + lane;
+#pragma unroll
+            for (int h = 0; h < 4; ++h) x[j][h] = op[h * 64];
+            ms[j] = s0 + j < S ? mp[(size_t)s * ROWS] : -INFINITY;
+            ls[j] = lp[(size_t)s * ROWS];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if (ms[j] == -INFINITY) continue;            // saw nothing
+            const float w = ms[j] == m ? 1.f : __builtin_amdgcn_exp2f(ms[j] - m);
+            den += w * ls[j];
+#pragma unroll
+            for (int h = 0; h < 4; ++h)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) num[h][e] += w * x[j][h][e];
+        }
+    }
+    if (f >= pl.f1) return;
+    const float inv = 1.f / den;
+    const int hq = f / d.R, r = f - hq * d.R;
+    bf16_t *out = (bf16_t *)c.out + (((size_t)pl.b * d.R + r) * c.n_q + pl.g * a.group + hq) * HD;
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+        if constexpr (KV4) {
+            if (h < 2)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    *(bf16x2 *)(out + 8 * (8 * h + 4 * lh + e) + 2 * t) = (bf16x2){(bf16_t)(num[h][e] * inv), (bf16_t)(num[h + 2][e] * inv)};
+        } else {
+            typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+            *(bf16x4 *)(out + 32 * t + 8 * h + 4 * lh) =
+                (bf16x4){(bf16_t)(num[h][0] * inv), (bf16_t)(num[h][1] * inv), (bf16_t)(num[h][2] * inv), (bf16_t)(num[h][3] * inv)};
+        }
+    }
+}
+
+int groups_of(const SpanArgs &a) { return a.c.B * (a.c.kv.k_pages ? a.c.kv.n_kv : a.c.kv4.n_kv); }
+
 }  // namespace
 
-void launch_span_rows(const SpanArgs &a, int chunks, hipStream_t st) {
-    const bool four = a.c.kv.k_pages == nullptr;
-    const dim3 grid(a.c.B * (four ? a.c.kv4.n_kv : a.c.kv.n_kv) * chunks, a.splits);
-    if (four) span_rows_kernel<true><<<grid, 256, 0, st>>>(a);
-    else span_rows_kernel<false><<<grid, 256, 0, st>>>(a);
+// Whole workgroups first, then the key splits of the rest: of every round but the last 512 workgroups, two to a compute unit, run at a
+// time.  The rest (fewer than 512) is cut into the number of splits that takes the least time, in iterations of about a microsecond
+// with two workgroups to a unit: eight for a workgroup's prologue, twelve more where its partial results (66 KB) go out and come
+// back; no more than 1024 workgroups and one per four iterations.  That bound sizes the workspace, which then depends
+// on the rows alone.
+void plan_span_rows(int B, int n_kv, int group, const RowDesc &d, int window, int sinks, int max_prefix, SpanPlan *p) {
+    const int F = group * d.R;
+    // rows of one head see one run of keys where they are many: chunks that run over the end of a head would walk all of them
+    p->span_rows = d.nc >= ROWS ? d.R : F;
+    p->tiles = F / p->span_rows * ((p->span_rows + ROWS - 1) / ROWS);
+    const int items = B * n_kv * p->tiles, rest = items % 512;
+    const int most = rest ? std::min(64, 1024 / rest) : 1;
+    const int iters = (int)((span_keys(d, p->span_rows == F ? d.R : ROWS, window, sinks, max_prefix) + 31) / 32);
+    p->splits = 1;
+    double best = 0.0;
+    for (int s = 1; s <= most && (s == 1 || 4 * s <= iters); ++s) {
+        const double t = (double)((rest * s + 511) / 512) * ((iters + s - 1) / s + (s == 1 ? 8 : 20));
+        if (s == 1 || t < 0.97 * best) {
+            best = t;
+            p->splits = s;
+        }
+    }
+    p->whole = p->splits == 1 ? items : items - rest;
+    p->part_floats = most > 1 ? (size_t)rest * most * ROWS * (HD + 2) : 0;
+}
+
+void launch_span_rows(const SpanArgs &a, hipStream_t st) {
+    const int items = groups_of(a) * a.tiles, grid = a.whole + (items - a.whole) * a.splits;
+    if (a.c.kv.k_pages) span_rows_kernel<false><<<grid, 256, 0, st>>>(a);
+    else span_rows_kernel<true><<<grid, 256, 0, st>>>(a);
+}
+
+void launch_span_rows_join(const SpanArgs &a, hipStream_t st) {
+    const int tail = groups_of(a) * a.tiles - a.whole;
+    if (a.c.kv.k_pages) span_rows_join_kernel<false><<<tail * 4, 256, 0, st>>>(a);
+    else span_rows_join_kernel<true><<<tail * 4, 256, 0, st>>>(a);
 }

@@ -427,16 +427,21 @@ struct SpanCall {
 };
 struct SpanPlan {
     bool rows;                 // many rows (kernels_span_rows.hip): 128 to a workgroup, else 16
+    int span_rows;             // workgroups of many rows do not run over a multiple of this: a query head's rows, or all of them
+    int whole;                 // and so many of them walk all of their keys, the others are cut into splits
     int tiles;                 // workgroups per kv head and key split
     int splits;                // of the keys
     size_t part_floats;
 };
 struct SpanArgs {
     SpanCall c;
-    int group, tiles, splits;
+    int group, tiles, splits, span_rows, whole;
     float *opart, *mpart, *lpart;
 };
-void launch_span_rows(const SpanArgs &a, int chunks, hipStream_t st);
+long long span_keys(const RowDesc &d, int rows, int window, int sinks, int max_prefix);
+void plan_span_rows(int B, int n_kv, int group, const RowDesc &d, int window, int sinks, int max_prefix, SpanPlan *p);
+void launch_span_rows(const SpanArgs &a, hipStream_t st);
+void launch_span_rows_join(const SpanArgs &a, hipStream_t st);
 SpanPlan plan_span(int dtype, int B, int n_q, int n_kv, int hd, const RowDesc &d, int window, int sinks, int max_prefix);
 void launch_span_attention(int dtype, const SpanCall &c, const SpanPlan &p, hipStream_t st);
 void launch_span_combine(int dtype, const SpanCall &c, const SpanPlan &p, hipStream_t st);
