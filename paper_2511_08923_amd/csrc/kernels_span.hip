@@ -58,8 +58,7 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
     if (!row) rs.hi = rs.lo = rs.sk = rs.m0 = rs.ms = rs.ml = rs.m1 = 0;
     const int n_it = fits ? wk.n1 + wk.n2 : 0, per = (n_it + a.splits - 1) / a.splits;
     const int it0 = min(n_it, split * per), it1 = min(n_it, it0 + per);
-    const __attribute__((address_space(4))) int32_t *pt = (const __attribute__((address_space(4))) int32_t *)(
-        (KV4 ? c.kv4.page_table : c.kv.page_table) + (size_t)(d.seq_base + b) * pps);
+    const int32_t *pt = (KV4 ? c.kv4.page_table : c.kv.page_table) + (size_t)(d.seq_base + b) * pps;
     const int n_mt = (d.nm + 15) >> 4;
     bool bad = !fits;                                    // a page id outside the pool: the rows come out as NaN
 
@@ -84,28 +83,41 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
     for (int t = 0; t < HT; ++t) acc[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
     float m_run = -INFINITY, l_run = 0.f;
 
-    // the unit (or -1) of walk position w
-    auto cache_unit = [&](int w) { return wk.cache_unit(w); };
-    auto page_of = [&](int u) {
-        int page = u >= 0 ? pt[u] : 0;
+    // Page ids of this wave's next 32 iterations, a lane each (0 for a unit that is not there): lane 2 i + t holds unit t's of its
+    // i-th iteration from `first` on.  (One scalar load per iteration had to be waited for in each, together with all of LDS.)
+    auto load_pages = [&](int first) {
+        const int w = 2 * (first + 4 * (lane >> 1)) + (lane & 1), u = wk.cache_unit(w);
+        int page = first + 4 * (lane >> 1) < it1 && u >= 0 ? pt[u] : 0;
         if ((unsigned)page >= (unsigned)n_pages) {
             bad = true;
             page = 0;
         }
         return page;
     };
+    int pages = 0, pages_at = 0;
+    auto page_of = [&](int n, int t) { return __builtin_amdgcn_readlane(pages, ((n - pages_at) >> 1) + t); };      // iteration n, unit t
+    auto pages_for = [&](int n) {                        // before iteration n's pages are asked for (n in steps of 4)
+        if (n - pages_at >= 128) {
+            pages = load_pages(n);
+            pages_at = n;
+        }
+    };
+    pages_at = it0 + wave;
+    pages = load_pages(pages_at);
+
     // softmax of one iteration's scores (two tiles of 16 keys; key of register e of tile t: bit key_bit(t, e))
     auto key_bit = [&](int t, int e) { return QUADS ? 16 * t + 4 * kg + e : 8 * kg + 4 * t + e; };
-    auto softmax = [&](auto masked_c, f32x4 (&s)[2], unsigned vis, float (&p)[8]) __attribute__((always_inline)) {
-        constexpr bool MASKED = decltype(masked_c)::value;
+    auto softmax = [&](bool whole, f32x4 (&s)[2], unsigned vis, float (&p)[8]) __attribute__((always_inline)) {
         float mx = -INFINITY;
+        if (!whole)
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) s[t][e] = ((vis >> key_bit(t, e)) & 1u) ? s[t][e] : -INFINITY;
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                if (MASKED) s[t][e] = ((vis >> key_bit(t, e)) & 1u) ? s[t][e] : -INFINITY;
-                mx = fmaxf(mx, s[t][e]);
-            }
+            for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[t][e]);
         if (__any(!(mx * scale <= m_run + kLag))) {      // rare: a row's first keys, or scores that outgrow the reference
             mx = fmaxf(mx, __shfl_xor(mx, 16));
             mx = fmaxf(mx, __shfl_xor(mx, 32));
@@ -129,8 +141,7 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
 
     if constexpr (BF) {
         // ---- bf16: 16x16x32 MFMAs
-        auto body = [&](auto masked_c, const bf16x8 (&kf)[2][4], bf16x8 (&vf)[HT], unsigned vis) __attribute__((always_inline)) {
-            constexpr bool MASKED = decltype(masked_c)::value;
+        auto body = [&](bool whole, const bf16x8 (&kf)[2][4], bf16x8 (&vf)[HT], unsigned vis) __attribute__((always_inline)) {
             f32x4 s[2];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
@@ -139,7 +150,7 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
                 for (int j = 0; j < 4; ++j) s[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[t][j], qb[j], s[t], 0, 0, 0);
             }
             float p[8];
-            softmax(masked_c, s, vis, p);
+            softmax(whole, s, vis, p);
             const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
             bf16x8 pf;
 #pragma unroll
@@ -149,7 +160,7 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
                 pf[e] = pk[0];
                 pf[e + 1] = pk[1];
             }
-            if (MASKED) {
+            if (!whole) {
                 unsigned odd = 0;
 #pragma unroll
                 for (int t = 0; t < HT; ++t) {
@@ -157,41 +168,30 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
                     odd |= nonfinite2(w[0]) | nonfinite2(w[1]) | nonfinite2(w[2]) | nonfinite2(w[3]);
                 }
                 if (__builtin_expect(__any(odd != 0), 0)) {
-                    // V without them, and for every (value, row) how many of each kind its visible keys hold
-                    bf16x8 seen;
+                    // taken out of the fragments, and added for the rows that see them, key by key through the wave's share of
+                    // LDS (rare, and written to need few registers)
+                    unsigned short *v = reinterpret_cast<unsigned short *>(&red[wave][0][0]);
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) seen[e] = (bf16_t)(float)((vis >> key_bit(e >> 2, e & 3)) & 1u);
+                    for (int t = 0; t < HT; ++t) *(bf16x8 *)(v + (16 * t + lq) * 32 + 8 * kg) = vf[t];
+#pragma unroll 1
+                    for (int i = 0; i < 32; ++i) {       // slot i % 8 of the lanes of quarter i / 8
+                        const int q8 = i >> 3, e = i & 7;
+                        const bool seen = (vis >> (QUADS ? 16 * (e >> 2) + 4 * q8 + (e & 3) : i)) & 1u;
 #pragma unroll
-                    for (int t = 0; t < HT; ++t) {
-                        bf16x8 pos, neg, nan, clean;
+                        for (int t = 0; t < HT; ++t)
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const float x = (float)vf[t][e];
-                            pos[e] = (bf16_t)(x == INFINITY ? 1.f : 0.f);
-                            neg[e] = (bf16_t)(x == -INFINITY ? 1.f : 0.f);
-                            nan[e] = (bf16_t)(x != x ? 1.f : 0.f);
-                            clean[e] = fabsf(x) < INFINITY ? vf[t][e] : (bf16_t)0.f;
-                        }
-                        const f32x4 z = {0.f, 0.f, 0.f, 0.f};
-                        const f32x4 n_pos = __builtin_amdgcn_mfma_f32_16x16x32_bf16(pos, seen, z, 0, 0, 0);
-                        const f32x4 n_neg = __builtin_amdgcn_mfma_f32_16x16x32_bf16(neg, seen, z, 0, 0, 0);
-                        const f32x4 n_nan = __builtin_amdgcn_mfma_f32_16x16x32_bf16(nan, seen, z, 0, 0, 0);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            if (n_pos[e] > 0.f) acc[t][e] += INFINITY;
-                            if (n_neg[e] > 0.f) acc[t][e] -= INFINITY;
-                            if (n_nan[e] > 0.f) acc[t][e] = __builtin_nanf("");
-                        }
-                        vf[t] = clean;
+                            for (int r4 = 0; r4 < 4; ++r4) {
+                                const float x = __uint_as_float((unsigned)v[(16 * t + 4 * kg + r4) * 32 + i] << 16);
+                                acc[t][r4] += seen && !(fabsf(x) < INFINITY) ? x : 0.f;
+                            }
                     }
+#pragma unroll
+                    for (int t = 0; t < HT; ++t) vf[t] = finite_only(vf[t]);
                 }
             }
 #pragma unroll
             for (int t = 0; t < HT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[t], pf, acc[t], 0, 0, 0);
         };
-        const std::true_type masked;
-        const std::false_type plain;
-
         // exact tiles, K [16][128] and V [128][16]: of a page or of the mask rows
         auto load_exact = [&](const bf16_t *k0, const bf16_t *k1, const bf16_t *v0, const bf16_t *v1, bf16x8 (&kf)[2][4],
                               bf16x8 (&vf)[HT]) __attribute__((always_inline)) {
@@ -219,56 +219,83 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
             }
         };
         auto mask_tile = [&](int u) { return ((((size_t)b * n_kv + g) * n_mt + max(u, 0)) * 16) * HD; };
-        int n = it0 + wave;
-        for (; n < min(it1, wk.n1); n += 4) {
-            const int u0 = cache_unit(2 * n), u1 = cache_unit(2 * n + 1);
-            bf16x8 kf[2][4], vf[HT];
+        // an iteration's codes (4-bit pages) or tiles (exact pages), asked for AHEAD iterations before they are needed
+        constexpr int AHEAD = KV4 ? 2 : 1;
+        struct Raw4 {
+            u32x4 k[2], v[2];
+            unsigned ks[2], vs[2];
+        };
+        struct RawExact {
+            bf16x8 k[2][4], v[HT];
+        };
+        typedef std::conditional_t<KV4, Raw4, RawExact> Raw;
+        auto fetch = [&](int n) __attribute__((always_inline)) {
+            Raw x;
+            pages_for(n);
             if constexpr (KV4) {
-                const unsigned char *p0 = c.kv4.pages + kv4_offset(c.kv4, page_of(u0), g);
-                const unsigned char *p1 = c.kv4.pages + kv4_offset(c.kv4, page_of(u1), g);
-                u32x4 kw[2], vw[2];
-                unsigned ks[2], vs[2];
-                const unsigned char *pp[2] = {p0, p1};
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    kw[t] = *(const u32x4 *)(pp[t] + kg * 256 + lq * 16);
-                    vw[t] = *(const u32x4 *)(pp[t] + kv4_v_codes(4) + kg * 256 + lq * 16);
-                    ks[t] = pp[t][kv4_k_scales(4) + kg * 16 + lq];
-                    vs[t] = *(const unsigned *)(pp[t] + kv4_v_scales(4) + (lq >> 2) * 16 + 4 * kg);
+                    const unsigned char *p = c.kv4.pages + kv4_offset(c.kv4, page_of(n, t), g);
+                    x.k[t] = *(const u32x4 *)(p + kg * 256 + lq * 16);
+                    x.v[t] = *(const u32x4 *)(p + kv4_v_codes(4) + kg * 256 + lq * 16);
+                    x.ks[t] = p[kv4_k_scales(4) + kg * 16 + lq];
+                    x.vs[t] = *(const unsigned *)(p + kv4_v_scales(4) + (lq >> 2) * 16 + 4 * kg);
                 }
+            } else {
+                const size_t o0 = ((size_t)page_of(n, 0) * n_kv + g) * 16 * HD, o1 = ((size_t)page_of(n, 1) * n_kv + g) * 16 * HD;
+                load_exact((const bf16_t *)c.kv.k_pages + o0, (const bf16_t *)c.kv.k_pages + o1,
+                           (const bf16_t *)c.kv.v_pages + o0, (const bf16_t *)c.kv.v_pages + o1, x.k, x.v);
+            }
+            return x;
+        };
+        auto block = [&](int n, Raw &x) __attribute__((always_inline)) {
+            const int u0 = wk.cache_unit(2 * n), u1 = wk.cache_unit(2 * n + 1);
+            const bool whole = all_see(rb, u0) && all_see(rb, u1);
+            const unsigned vis = whole ? ~0u : cache_bits(rs, u0) | (cache_bits(rs, u1) << 16);
+            if constexpr (KV4) {
+                bf16x8 kf[2][4], vf[HT];
 #pragma unroll
                 for (int t = 0; t < 2; ++t) {
-                    const float s = kv4_scale(ks[t]);
+                    const float s = kv4_scale(x.ks[t]);
 #pragma unroll
                     for (int j = 0; j < 4; ++j) {
-                        const bf16x2 x0 = kv4_pair_bf16<0>(kw[t][j], s), x1 = kv4_pair_bf16<1>(kw[t][j], s),
-                                     x2 = kv4_pair_bf16<2>(kw[t][j], s), x3 = kv4_pair_bf16<3>(kw[t][j], s);
+                        const bf16x2 x0 = kv4_pair_bf16<0>(x.k[t][j], s), x1 = kv4_pair_bf16<1>(x.k[t][j], s),
+                                     x2 = kv4_pair_bf16<2>(x.k[t][j], s), x3 = kv4_pair_bf16<3>(x.k[t][j], s);
                         kf[t][j] = (bf16x8){x0[0], x0[1], x1[0], x1[1], x2[0], x2[1], x3[0], x3[1]};
                     }
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {        // token 4 kg + e: eight head-dim values of lane lq
-                        const float sv = kv4_scale((vs[t] >> (8 * e)) & 255u);
-                        const bf16x2 x0 = kv4_pair_bf16<0>(vw[t][e], sv), x1 = kv4_pair_bf16<1>(vw[t][e], sv),
-                                     x2 = kv4_pair_bf16<2>(vw[t][e], sv), x3 = kv4_pair_bf16<3>(vw[t][e], sv);
+                        const float sv = kv4_scale((x.vs[t] >> (8 * e)) & 255u);
+                        const bf16x2 x0 = kv4_pair_bf16<0>(x.v[t][e], sv), x1 = kv4_pair_bf16<1>(x.v[t][e], sv),
+                                     x2 = kv4_pair_bf16<2>(x.v[t][e], sv), x3 = kv4_pair_bf16<3>(x.v[t][e], sv);
                         const int at = 4 * t + e;
                         vf[0][at] = x0[0]; vf[1][at] = x0[1]; vf[2][at] = x1[0]; vf[3][at] = x1[1];
                         vf[4][at] = x2[0]; vf[5][at] = x2[1]; vf[6][at] = x3[0]; vf[7][at] = x3[1];
                     }
                 }
+                body(whole, kf, vf, vis);
             } else {
-                const size_t o0 = ((size_t)page_of(u0) * n_kv + g) * 16 * HD, o1 = ((size_t)page_of(u1) * n_kv + g) * 16 * HD;
-                load_exact((const bf16_t *)c.kv.k_pages + o0, (const bf16_t *)c.kv.k_pages + o1,
-                           (const bf16_t *)c.kv.v_pages + o0, (const bf16_t *)c.kv.v_pages + o1, kf, vf);
+                body(whole, x.k, x.v, vis);
             }
-            if (all_see(rb, u0) && all_see(rb, u1)) body(plain, kf, vf, ~0u);
-            else body(masked, kf, vf, cache_bits(rs, u0) | (cache_bits(rs, u1) << 16));
+        };
+        const int end1 = min(it1, wk.n1);
+        int n = it0 + wave;
+        if (n < end1) {
+            Raw x0 = fetch(n), x1;
+            if (AHEAD == 2 && n + 4 < end1) x1 = fetch(n + 4);
+            for (; n < end1; n += 4) {
+                Raw now = x0;
+                if constexpr (AHEAD == 2) x0 = x1;
+                if (n + 4 * AHEAD < end1) (AHEAD == 2 ? x1 : x0) = fetch(n + 4 * AHEAD);
+                block(n, now);
+            }
         }
         for (; n < it1; n += 4) {
             const int w = 2 * (n - wk.n1), u0 = wk.mask_unit(w), u1 = wk.mask_unit(w + 1);
             bf16x8 kf[2][4], vf[HT];
             load_exact((const bf16_t *)c.k_scr + mask_tile(u0), (const bf16_t *)c.k_scr + mask_tile(u1),
                        (const bf16_t *)c.v_scr + mask_tile(u0), (const bf16_t *)c.v_scr + mask_tile(u1), kf, vf);
-            body(masked, kf, vf, mask_bits(rs, u0) | (mask_bits(rs, u1) << 16));
+            body(false, kf, vf, mask_bits(rs, u0) | (mask_bits(rs, u1) << 16));
         }
     } else {
         // ---- fp32: 16x16x4 MFMAs.  A lane's head-dim values of O^T tile t are HT i + t.
@@ -372,13 +399,14 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
         for (int n = it0 + wave; n < it1; n += 4) {
             const bool cache = n < wk.n1;
             const int w = cache ? 2 * n : 2 * (n - wk.n1);
-            const int u[2] = {cache ? cache_unit(w) : wk.mask_unit(w), cache ? cache_unit(w + 1) : wk.mask_unit(w + 1)};
+            const int u[2] = {cache ? wk.cache_unit(w) : wk.mask_unit(w), cache ? wk.cache_unit(w + 1) : wk.mask_unit(w + 1)};
+            pages_for(n);
             size_t at[2];
             f32x4 s[2], v[HT];
             float k[Q4], p[8];
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-                const size_t piece = cache ? (size_t)page_of(u[t]) * n_kv + g : ((size_t)b * n_kv + g) * n_mt + max(u[t], 0);
+                const size_t piece = cache ? (size_t)page_of(n, t) * n_kv + g : ((size_t)b * n_kv + g) * n_mt + max(u[t], 0);
                 at[t] = piece * 16 * hd;
                 if (KV4 && cache) load_k4(c.kv4.pages + piece * kv4_head_bytes(hd), k);
                 else load_k((const float *)(cache ? c.kv.k_pages : c.k_scr) + at[t], k);
@@ -386,7 +414,7 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
                 s[t] = scores(k);
             }
             const unsigned vis = cache ? cache_bits(rs, u[0]) | (cache_bits(rs, u[1]) << 16) : mask_bits(rs, u[0]) | (mask_bits(rs, u[1]) << 16);
-            softmax(std::true_type(), s, vis, p);
+            softmax(false, s, vis, p);
 #pragma unroll
             for (int e = 0; e < 8; ++e) l_run += p[e];
 #pragma unroll
@@ -402,7 +430,7 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
     float l = l_run;
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
-    if (bad) {
+    if (__any(bad)) {
         l = __builtin_nanf("");
         if (m_run == -INFINITY) m_run = 0.f;
     }

@@ -298,15 +298,7 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
 #pragma unroll
             for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    u32x4 w = __builtin_bit_cast(u32x4, vf[t][u]);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        if ((w[i] & 0x7f80u) == 0x7f80u) w[i] &= 0xffff0000u;
-                        if ((w[i] & 0x7f800000u) == 0x7f800000u) w[i] &= 0xffffu;
-                    }
-                    vf[t][u] = __builtin_bit_cast(bf16x8, w);
-                }
+                for (int u = 0; u < 2; ++u) vf[t][u] = finite_only(vf[t][u]);
         }
     };
 

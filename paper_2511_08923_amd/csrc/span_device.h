@@ -98,6 +98,16 @@ __device__ inline unsigned mask_bits(const RowSpan &s, int u) {
     return u < 0 ? 0u : bits16(s.ml - 16 * u, s.m1 - 16 * u) | bits16(s.m0 - 16 * u, s.ms - 16 * u);
 }
 
+// of two bf16 values: bits where one is not finite; and zeros in the places of those
 __device__ inline unsigned nonfinite2(unsigned x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+__device__ inline bf16x8 finite_only(bf16x8 v) {
+    u32x4 w = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if ((w[i] & 0x7f80u) == 0x7f80u) w[i] &= 0xffff0000u;
+        if ((w[i] & 0x7f800000u) == 0x7f800000u) w[i] &= 0xffffu;
+    }
+    return __builtin_bit_cast(bf16x8, w);
+}
 
 }  // namespace
