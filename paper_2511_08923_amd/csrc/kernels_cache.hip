@@ -10,7 +10,7 @@ namespace {
 // free list (or none), in the order of the sequences.  Where a sequence's pages begin in the list, and its rows in the
 // slot map, is an exclusive sum over the sequences before it.  Every workgroup adds up its predecessors by itself, so the
 // whole is one launch: up to 512 workgroups read 8 bytes of each predecessor from L2 (batch 2048: 12 MB in all), which is less than
-// the second launch that a scan in two steps costs.  A wave then takes a sequence at a time.
+// the second launch that a scan in two steps costs.  A wave then takes a sequence at a time, its pages a lane each.
 struct TableArgs {
     int batch;
     const int32_t *prefix_len, *n_new, *held, *free_pages;
@@ -40,46 +40,40 @@ __device__ inline SeqNeed seq_need(const TableArgs &a, int b) {
     return s;
 }
 __device__ inline int saturate(long long v) { return v > 0x7fffffff ? 0x7fffffff : (int)v; }
-__device__ inline bool fits(const TableArgs &a, long long off, int need, int rows, long long rows_end) {
-    return (need == 0 || off + need <= a.n_free) && (rows == 0 || rows_end <= a.slot_cap);
-}
-
 __global__ __launch_bounds__(256) void table_extend_kernel(TableArgs a) {
-    __shared__ long long sum_need[256], sum_rows[256];
+    __shared__ long long sum_need[256], sum_rows[256];    // inclusive, of a run of up to 256 sequences
+    __shared__ SeqNeed seqs[256];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int b0 = blockIdx.x * a.per_wg, b1 = min(a.batch, b0 + a.per_wg);
-    const bool last = b1 == a.batch;
-    // sums over a range of sequences, in every thread
-    auto total = [&](int lo, int hi, long long &need, long long &rows) {
-        long long x = 0, y = 0;
-        for (int b = lo + tid; b < hi; b += 256) {
-            const SeqNeed s = seq_need(a, b);
-            x += s.need;
-            y += s.n;
-        }
+    // what the sequences before this workgroup's need, and their rows
+    long long base_need = 0, base_rows = 0;
+    for (int b = tid; b < b0; b += 256) {
+        const SeqNeed s = seq_need(a, b);
+        base_need += s.need;
+        base_rows += s.n;
+    }
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            x += __shfl_xor(x, o);
-            y += __shfl_xor(y, o);
-        }
-        __syncthreads();
-        if (lane == 0) {
-            sum_need[wave] = x;
-            sum_rows[wave] = y;
-        }
-        __syncthreads();
-        need = sum_need[0] + sum_need[1] + sum_need[2] + sum_need[3];
-        rows = sum_rows[0] + sum_rows[1] + sum_rows[2] + sum_rows[3];
-        __syncthreads();
-    };
-    long long base_need, base_rows;
-    total(0, b0, base_need, base_rows);
-    long long taken = 0;
+    for (int o = 1; o < 64; o <<= 1) {
+        base_need += __shfl_xor(base_need, o);
+        base_rows += __shfl_xor(base_rows, o);
+    }
+    if (lane == 0) {
+        sum_need[wave] = base_need;
+        sum_rows[wave] = base_rows;
+    }
+    __syncthreads();
+    base_need = sum_need[0] + sum_need[1] + sum_need[2] + sum_need[3];
+    base_rows = sum_rows[0] + sum_rows[1] + sum_rows[2] + sum_rows[3];
+    // The sequences whose pages the list has and whose rows the slot map has are the first ones (both sums only grow), and so
+    // what the list has lost is what they need together: the workgroup that they end in writes it
+    const bool was_in = base_need <= a.n_free && base_rows <= a.slot_cap;
+    long long taken = base_need;
     for (int c0 = b0; c0 < b1; c0 += 256) {
         const int m = min(256, b1 - c0);
-        // inclusive sums of this run of sequences
+        __syncthreads();
         SeqNeed mine = {};
         if (tid < m) mine = seq_need(a, c0 + tid);
+        seqs[tid] = mine;
         long long x = mine.need, y = mine.n;
 #pragma unroll
         for (int o = 1; o < 64; o <<= 1) {
@@ -99,30 +93,42 @@ __global__ __launch_bounds__(256) void table_extend_kernel(TableArgs a) {
         __syncthreads();
         sum_need[tid] = x;
         sum_rows[tid] = y;
+        if (tid < m && base_need + x <= a.n_free && base_rows + y <= a.slot_cap) taken = max(taken, base_need + x);
         __syncthreads();
-        for (int i = wave; i < m; i += 4) {
+        for (int i = wave; i < m; i += 4) {               // a wave to a sequence
             const int b = c0 + i;
-            const SeqNeed s = seq_need(a, b);
+            const SeqNeed s = seqs[i];
             const long long off = base_need + sum_need[i] - s.need;
             const long long row0 = base_rows + sum_rows[i] - s.n, row1 = row0 + s.n;
             int32_t *table = a.page_table + (size_t)b * a.pages_per_seq;
-            const bool room = s.ok && fits(a, off, s.need, s.n, row1);
-            // the pages that the new rows go into: those that the sequence has, and those from the list
+            const bool room = s.ok && (s.need == 0 || off + s.need <= a.n_free) && (s.n == 0 || row1 <= a.slot_cap);
+            // the pages that the new rows go into: those that the sequence has, and those from the list; a lane each
+            const int first = s.P >> 4, pages = s.n > 0 ? ((s.P + s.n + 15) >> 4) - first : 0;
+            auto page_of = [&](int j) {                   // logical page first + j
+                const int lp = first + j;
+                return lp < s.held ? table[lp] : a.free_pages[off + (lp - s.held)];
+            };
             bool ids = true;
-            const int first = s.P >> 4, own_end = min(s.held, (s.P + s.n + 15) >> 4);
-            if (room && s.n > 0)
-                for (int j = first + lane; j < own_end; j += 64) ids = ids && (unsigned)table[j] < (unsigned)a.n_pages;
+            int page = 0;
             if (room)
-                for (int j = lane; j < s.need; j += 64) ids = ids && (unsigned)a.free_pages[off + j] < (unsigned)a.n_pages;
+                for (int j = lane; j < pages; j += 64) {
+                    const int p = page_of(j);
+                    if (j < 64) page = p;
+                    ids = ids && (unsigned)p < (unsigned)a.n_pages;
+                }
             ids = __all(ids);
             const int granted = !s.ok ? -1 : !room ? 0 : ids ? 1 : -1;
-            if (granted == 1)
-                for (int j = lane; j < s.need; j += 64) table[s.held + j] = a.free_pages[off + j];
-            for (long long r = row0 + lane; r < row1 && r < a.slot_cap; r += 64) {
-                const int p = s.P + (int)(r - row0), lp = p >> 4;
-                int slot = -1;
-                if (granted == 1) slot = (lp < s.held ? table[lp] : a.free_pages[off + (lp - s.held)]) * 16 + (p & 15);
-                a.slots[r] = slot;
+            for (int j0 = 0; j0 == 0 || j0 < pages; j0 += 64) {
+                const int j = j0 + lane;
+                if (j0 > 0 && granted == 1 && j < pages) page = page_of(j);
+                if (granted == 1 && j < pages && first + j >= s.held) table[first + j] = page;
+                // rows of these 64 pages
+                const int p0 = max(s.P, 16 * (first + j0)), p1 = min(s.P + s.n, 16 * (first + j0 + 64));
+                for (int p = p0; p < p1; p += 64) {       // (uniform, for the shuffle)
+                    const int at = p + lane, slot = __shfl(page, (at >> 4) - first - j0) * 16 + (at & 15);
+                    const long long r = row0 + (at - s.P);
+                    if (at < p1 && r < a.slot_cap) a.slots[r] = granted == 1 ? slot : -1;
+                }
             }
             if (lane == 0) {
                 a.granted[b] = granted;
@@ -130,68 +136,20 @@ __global__ __launch_bounds__(256) void table_extend_kernel(TableArgs a) {
                 a.row_start[b + 1] = saturate(row1);
             }
         }
-        // what the list has lost: the furthest end of a valid sequence that it had room for
-        if (tid < m && mine.need > 0 && fits(a, base_need + x - mine.need, mine.need, mine.n, base_rows + y)) {
-            const long long end = base_need + x;
-            taken = end > taken ? end : taken;
-        }
-        const long long n_need = sum_need[m - 1], n_rows = sum_rows[m - 1];
-        __syncthreads();
-        base_need += n_need;
-        base_rows += n_rows;
+        base_need += sum_need[m - 1];
+        base_rows += sum_rows[m - 1];
     }
+    const bool is_in = base_need <= a.n_free && base_rows <= a.slot_cap, last = b1 == a.batch;
     if (blockIdx.x == 0 && tid == 0) a.row_start[0] = 0;
-    if (!last) return;
-    for (long long r = base_rows + tid; r < a.slot_cap; r += 256) a.slots[r] = -1;       // padding of the slot map
-    // n_taken needs every sequence: ends only grow, so the largest that fits is found by one more pass over those before
-    long long run_need = 0, run_rows = 0;
-    for (int c0 = 0; c0 < b0; c0 += 256) {
-        const int m = min(256, b0 - c0);
-        SeqNeed mine = {};
-        if (tid < m) mine = seq_need(a, c0 + tid);
-        long long x = mine.need, y = mine.n;
+    if (last)                                             // padding of the slot map
+        for (long long r = base_rows + tid; r < a.slot_cap; r += 256) a.slots[r] = -1;
+    if (!was_in || (is_in && !last)) return;
 #pragma unroll
-        for (int o = 1; o < 64; o <<= 1) {
-            const long long px = __shfl_up(x, o), py = __shfl_up(y, o);
-            if (lane >= o) {
-                x += px;
-                y += py;
-            }
-        }
-        __syncthreads();
-        if (lane == 63) {
-            sum_need[wave] = x;
-            sum_rows[wave] = y;
-        }
-        __syncthreads();
-        long long all_need = 0, all_rows = 0;
-        for (int w = 0; w < 4; ++w) {
-            if (w < wave) {
-                x += sum_need[w];
-                y += sum_rows[w];
-            }
-            all_need += sum_need[w];
-            all_rows += sum_rows[w];
-        }
-        if (tid < m && mine.need > 0 && fits(a, run_need + x - mine.need, mine.need, mine.n, run_rows + y)) {
-            const long long end = run_need + x;
-            taken = end > taken ? end : taken;
-        }
-        run_need += all_need;
-        run_rows += all_rows;
-    }
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const long long t = __shfl_xor(taken, o);
-        taken = t > taken ? t : taken;
-    }
+    for (int o = 1; o < 64; o <<= 1) taken = max(taken, __shfl_xor(taken, o));
     __syncthreads();
     if (lane == 0) sum_need[wave] = taken;
     __syncthreads();
-    if (tid == 0) {
-        for (int w = 1; w < 4; ++w) taken = sum_need[w] > taken ? sum_need[w] : taken;
-        a.n_taken[0] = (int)taken;
-    }
+    if (tid == 0) a.n_taken[0] = (int)max(max(sum_need[0], sum_need[1]), max(sum_need[2], sum_need[3]));
 }
 
 // ------------------------------------------------------------------ rows into 4-bit pages and back
@@ -244,34 +202,39 @@ __global__ __launch_bounds__(256) void kv4_store_kernel(RowArgs a, const T *__re
     int row, h, grp;
     const bool here = row_piece(a, idx, row, h, grp);
     const int slot = here ? a.slots[row] : -1;
-    const bool ok = slot >= 0 && slot < (long long)a.kv.n_pages * 16;
-    const T *src = blockIdx.y ? v : k;
-    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    float x[2][8] = {};
     const int n = hd - 8 * grp;                           // elements of this group that there are
-    if (ok && n > 0) load8(src + ((size_t)row * a.kv.n_kv + h) * hd + 8 * grp, n, a.vec && n >= 8, x);
-    unsigned amax = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) amax = max(amax, __float_as_uint(x[e]) & 0x7fffffffu);
-    amax = max(amax, (unsigned)__shfl_xor((int)amax, 1));
-    amax = max(amax, (unsigned)__shfl_xor((int)amax, 2));
-    if (!ok) return;
-    const unsigned byte = kv4_scale_byte(amax);
-    unsigned codes = 0x77777777u;                         // of a block that reads back as NaN
-    if (byte != kScaleNan) {
-        const float scale = kv4_scale(byte);
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, x[0], x[1], scale, 0);
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[2], x[3], scale, 1);
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[4], x[5], scale, 2);
-        codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, x[6], x[7], scale, 3);
+    if (here && n > 0) {                                  // (whatever the slot: one trip to memory for all three)
+        const size_t src = ((size_t)row * a.kv.n_kv + h) * hd + 8 * grp;
+        load8(k + src, n, a.vec && n >= 8, x[0]);
+        load8(v + src, n, a.vec && n >= 8, x[1]);
     }
+    unsigned codes[2], byte[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        unsigned amax = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) amax = max(amax, __float_as_uint(x[i][e]) & 0x7fffffffu);
+        amax = max(amax, (unsigned)__shfl_xor((int)amax, 1));
+        amax = max(amax, (unsigned)__shfl_xor((int)amax, 2));
+        byte[i] = kv4_scale_byte(amax);
+        codes[i] = 0x77777777u;                           // of a block that reads back as NaN
+        if (byte[i] != kScaleNan) {
+            const float scale = kv4_scale(byte[i]);
+            codes[i] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, x[i][0], x[i][1], scale, 0);
+            codes[i] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes[i], x[i][2], x[i][3], scale, 1);
+            codes[i] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes[i], x[i][4], x[i][5], scale, 2);
+            codes[i] = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes[i], x[i][6], x[i][7], scale, 3);
+        }
+    }
+    if (slot < 0 || slot >= (long long)a.kv.n_pages * 16) return;
     unsigned char *blk = a.kv.pages + kv4_offset(a.kv, slot >> 4, h);
     const int t = slot & 15, b = grp >> 2;
-    if (blockIdx.y == 0) {
-        *(unsigned *)(blk + b * 256 + t * 16 + (grp & 3) * 4) = codes;
-        if ((grp & 3) == 0) blk[kv4_k_scales(nb) + b * 16 + t] = (unsigned char)byte;
-    } else {
-        *(unsigned *)(blk + kv4_v_codes(nb) + ((t >> 2) * 4 * nb + grp) * 16 + (t & 3) * 4) = codes;
-        if ((grp & 3) == 0) blk[kv4_v_scales(nb) + b * 16 + t] = (unsigned char)byte;
+    *(unsigned *)(blk + b * 256 + t * 16 + (grp & 3) * 4) = codes[0];
+    *(unsigned *)(blk + kv4_v_codes(nb) + ((t >> 2) * 4 * nb + grp) * 16 + (t & 3) * 4) = codes[1];
+    if ((grp & 3) == 0) {
+        blk[kv4_k_scales(nb) + b * 16 + t] = (unsigned char)byte[0];
+        blk[kv4_v_scales(nb) + b * 16 + t] = (unsigned char)byte[1];
     }
 }
 
@@ -284,33 +247,38 @@ __global__ __launch_bounds__(256) void kv4_load_kernel(RowArgs a, T *__restrict_
     const int n = hd - 8 * grp;
     if (n <= 0) return;
     const int slot = a.slots[row];
-    float x[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (slot >= 0 && slot < (long long)a.kv.n_pages * 16) {
+    const bool ok = slot >= 0 && slot < (long long)a.kv.n_pages * 16;
+    unsigned words[2] = {0, 0}, bytes[2] = {0, 0};
+    if (ok) {
         const unsigned char *blk = a.kv.pages + kv4_offset(a.kv, slot >> 4, h);
         const int t = slot & 15, b = grp >> 2;
-        const unsigned word = blockIdx.y ? *(const unsigned *)(blk + kv4_v_codes(nb) + ((t >> 2) * 4 * nb + grp) * 16 + (t & 3) * 4)
-                                         : *(const unsigned *)(blk + b * 256 + t * 16 + (grp & 3) * 4);
-        const unsigned byte = blk[(blockIdx.y ? kv4_v_scales(nb) : kv4_k_scales(nb)) + b * 16 + t];
-        const float s = kv4_scale(byte);
-        const kv4_f32x2 p0 = kv4_pair_f32<0>(word, s), p1 = kv4_pair_f32<1>(word, s), p2 = kv4_pair_f32<2>(word, s),
-                        p3 = kv4_pair_f32<3>(word, s);
-        const float y[8] = {p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = byte == kScaleNan ? __builtin_nanf("") : y[e];
+        words[0] = *(const unsigned *)(blk + b * 256 + t * 16 + (grp & 3) * 4);
+        words[1] = *(const unsigned *)(blk + kv4_v_codes(nb) + ((t >> 2) * 4 * nb + grp) * 16 + (t & 3) * 4);
+        bytes[0] = blk[kv4_k_scales(nb) + b * 16 + t];
+        bytes[1] = blk[kv4_v_scales(nb) + b * 16 + t];
     }
-    T *dst = (blockIdx.y ? v : k) + ((size_t)row * a.kv.n_kv + h) * hd + 8 * grp;
-    if (a.vec && n >= 8) {
-        if constexpr (sizeof(T) == 2) {
-            bf16x8 o;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = (bf16_t)x[e];
-            *(bf16x8 *)dst = o;
+    for (int i = 0; i < 2; ++i) {
+        const float s = kv4_scale(bytes[i]);
+        const kv4_f32x2 p0 = kv4_pair_f32<0>(words[i], s), p1 = kv4_pair_f32<1>(words[i], s), p2 = kv4_pair_f32<2>(words[i], s),
+                        p3 = kv4_pair_f32<3>(words[i], s);
+        float x[8] = {p0[0], p0[1], p1[0], p1[1], p2[0], p2[1], p3[0], p3[1]};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = !ok ? 0.f : bytes[i] == kScaleNan ? __builtin_nanf("") : x[e];
+        T *dst = (i ? v : k) + ((size_t)row * a.kv.n_kv + h) * hd + 8 * grp;
+        if (a.vec && n >= 8) {
+            if constexpr (sizeof(T) == 2) {
+                bf16x8 o;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) o[e] = (bf16_t)x[e];
+                *(bf16x8 *)dst = o;
+            } else {
+                *(f32x4 *)dst = (f32x4){x[0], x[1], x[2], x[3]};
+                *(f32x4 *)(dst + 4) = (f32x4){x[4], x[5], x[6], x[7]};
+            }
         } else {
-            *(f32x4 *)dst = (f32x4){x[0], x[1], x[2], x[3]};
-            *(f32x4 *)(dst + 4) = (f32x4){x[4], x[5], x[6], x[7]};
+            for (int e = 0; e < 8 && e < n; ++e) dst[e] = (T)x[e];
         }
-    } else {
-        for (int e = 0; e < 8 && e < n; ++e) dst[e] = (T)x[e];
     }
 }
 
@@ -417,7 +385,7 @@ static RowArgs row_args(const Kv4View &kv, const int32_t *slots, int n_rows, con
 }
 static dim3 row_grid(const Kv4View &kv, int n_rows) {
     const size_t lanes = (size_t)((n_rows + 3) / 4) * 4 * kv.n_kv * 4 * kv4_blocks(kv.hd);
-    return dim3((unsigned)((lanes + 255) / 256), 2);
+    return dim3((unsigned)((lanes + 255) / 256));
 }
 void launch_kv4_store(int dtype, const Kv4View &kv, const int32_t *slots, int n_rows, const void *k, const void *v,
                       hipStream_t st) {
