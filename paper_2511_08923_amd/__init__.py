@@ -144,18 +144,21 @@ def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
 
 def _stream() -> int:
     # the handle alone: torch.cuda.current_stream() builds a Stream object around it, 2.9 us of a call's host time against 0.3
-    return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+    return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
 
 
 class tidar_ctx(C.c_void_p):
-    """The library's handle; carries the configuration it was made from."""
-    cfg: tidar_config
+    """The library's handle; knows the type and the row sizes of the configuration it was made from."""
+    tdtype: torch.dtype
+    q_dim: int
+    kv_dim: int
 
 
 # ---------------------------------------------------------------- functions named after the C entry points
 def tidar_create(cfg: tidar_config) -> tidar_ctx:
     h = tidar_ctx()
-    h.cfg = cfg
+    h.tdtype = torch.bfloat16 if cfg.dtype == TIDAR_BF16 else torch.float32
+    h.q_dim, h.kv_dim = cfg.n_q_heads * cfg.head_dim, cfg.n_kv_heads * cfg.head_dim
     _check(_lib.tidar_create(C.byref(cfg), C.byref(h)), "tidar_create")
     return h
 
@@ -265,9 +268,6 @@ def tidar_score(ctx, w: tidar_weights, kv: tidar_kv_cache, batch: int, tokens: t
 
 # The calls around the cache check their tensors: a view with other strides, another type or device, or one that is too small
 # is refused (ValueError) before anything is enqueued.
-_DTYPE = {TIDAR_F32: torch.float32, TIDAR_BF16: torch.bfloat16}
-
-
 def _refuse(name: str, t: torch.Tensor, dtype: Optional[torch.dtype], numel: int, dev: int) -> None:
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{name}: {t.dtype}, expected {dtype}")
@@ -285,7 +285,10 @@ def _mem(name: str, t: torch.Tensor, dtype: Optional[torch.dtype], numel: int, d
 
 
 def _device() -> int:
-    return torch.cuda.current_device() if torch.cuda.is_available() else 0      # (no GPU: every tensor is refused)
+    try:
+        return torch._C._cuda_getDevice()
+    except RuntimeError:                                   # no GPU: every tensor is refused
+        return 0
 
 
 def tidar_table_extend(ctx: tidar_ctx, batch: int, prefix_len: torch.Tensor, n_new: torch.Tensor, held: torch.Tensor,
@@ -308,8 +311,7 @@ def tidar_kv4_page_bytes(ctx: tidar_ctx) -> int:
 
 
 def _kv4_rows(fn, where: str, ctx: tidar_ctx, kv, layer: int, n_rows: int, slots, k, v) -> None:
-    c, dev = ctx.cfg, _device()
-    dt, n = _DTYPE[c.dtype], n_rows * c.n_kv_heads * c.head_dim
+    dt, n, dev = ctx.tdtype, n_rows * ctx.kv_dim, _device()
     _check(fn(ctx, C.byref(kv), layer, n_rows, _mem("slots", slots, torch.int32, n_rows, dev), _mem("k", k, dt, n, dev),
               _mem("v", v, dt, n, dev), _stream()), where)
 
@@ -326,9 +328,8 @@ def tidar_kv4_load(ctx: tidar_ctx, kv: tidar_kv4_cache, layer: int, n_rows: int,
 
 def _span_attention(fn, where: str, ctx: tidar_ctx, kv, layer, batch, prefix_len, q, k_new, v_new, new_rows, n_causal,
                     n_blocks, block_len, cond0, window, sinks, out, hint, ws) -> None:
-    c, dev = ctx.cfg, _device()
-    dt, n_q = _DTYPE[c.dtype], batch * (n_causal + n_blocks * block_len) * c.n_q_heads * c.head_dim
-    n_kv = batch * new_rows * c.n_kv_heads * c.head_dim
+    dt, dev, rows = ctx.tdtype, _device(), batch * (n_causal + n_blocks * block_len)
+    n_q, n_kv = rows * ctx.q_dim, batch * new_rows * ctx.kv_dim
     _check(fn(ctx, C.byref(kv), layer, batch, _mem("prefix_len", prefix_len, torch.int32, batch, dev),
               _mem("q", q, dt, n_q, dev), None if k_new is None else _mem("k", k_new, dt, n_kv, dev),
               None if v_new is None else _mem("v", v_new, dt, n_kv, dev), n_causal, n_blocks, block_len, cond0, window, sinks,

@@ -238,7 +238,8 @@ __global__ __launch_bounds__(256) void kv4_store_kernel(RowArgs a, const T *__re
     }
 }
 
-template <typename T>
+// ONCE: more than the L2s hold together, written past them (16000 rows of 8 heads: 16.1 -> 13.4 us)
+template <typename T, bool ONCE>
 __global__ __launch_bounds__(256) void kv4_load_kernel(RowArgs a, T *__restrict__ k, T *__restrict__ v) {
     const int nb = kv4_blocks(a.kv.hd), hd = a.kv.hd;
     const size_t idx = (size_t)blockIdx.x * 256 + threadIdx.x;
@@ -271,7 +272,8 @@ __global__ __launch_bounds__(256) void kv4_load_kernel(RowArgs a, T *__restrict_
                 bf16x8 o;
 #pragma unroll
                 for (int e = 0; e < 8; ++e) o[e] = (bf16_t)x[e];
-                *(bf16x8 *)dst = o;
+                if constexpr (ONCE) __builtin_nontemporal_store(o, (bf16x8 *)dst);
+                else *(bf16x8 *)dst = o;
             } else {
                 *(f32x4 *)dst = (f32x4){x[0], x[1], x[2], x[3]};
                 *(f32x4 *)(dst + 4) = (f32x4){x[4], x[5], x[6], x[7]};
@@ -395,6 +397,8 @@ void launch_kv4_store(int dtype, const Kv4View &kv, const int32_t *slots, int n_
 }
 void launch_kv4_load(int dtype, const Kv4View &kv, const int32_t *slots, int n_rows, void *k, void *v, hipStream_t st) {
     const RowArgs a = row_args(kv, slots, n_rows, k, v);
-    if (dtype == TIDAR_BF16) kv4_load_kernel<<<row_grid(kv, n_rows), 256, 0, st>>>(a, (bf16_t *)k, (bf16_t *)v);
-    else kv4_load_kernel<<<row_grid(kv, n_rows), 256, 0, st>>>(a, (float *)k, (float *)v);
+    const bool once = (size_t)n_rows * kv.n_kv * kv.hd * 4 > 32u << 20;
+    if (dtype == TIDAR_BF16 && once) kv4_load_kernel<bf16_t, true><<<row_grid(kv, n_rows), 256, 0, st>>>(a, (bf16_t *)k, (bf16_t *)v);
+    else if (dtype == TIDAR_BF16) kv4_load_kernel<bf16_t, false><<<row_grid(kv, n_rows), 256, 0, st>>>(a, (bf16_t *)k, (bf16_t *)v);
+    else kv4_load_kernel<float, false><<<row_grid(kv, n_rows), 256, 0, st>>>(a, (float *)k, (float *)v);
 }

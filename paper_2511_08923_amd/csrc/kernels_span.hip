@@ -139,6 +139,21 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
             for (int e = 0; e < 4; ++e) p[4 * t + e] = __builtin_amdgcn_exp2f(fmaf(s[t][e], scale, -m_safe));
     };
 
+    // The one-token step: the new row's K/V are not in the cache yet.  The wave whose iteration holds position L takes them from
+    // where they are instead of its slot (which nobody else sees), and stores them.
+    const int new_unit = !KV4 && c.k_one ? L >> 4 : -2;
+    const size_t new_row = ((size_t)b * n_kv + g) * hd;
+    auto store_new = [&]() {
+        const int page = pt[L >> 4];
+        if ((unsigned)page >= (unsigned)n_pages) return;
+        const size_t at = ((size_t)page * n_kv + g) * 16 * hd;
+        T *kd = (T *)const_cast<void *>(c.kv.k_pages) + at + (L & 15) * hd, *vd = (T *)const_cast<void *>(c.kv.v_pages) + at + (L & 15);
+        for (int e = lane; e < hd; e += 64) {
+            kd[e] = ((const T *)c.k_one)[new_row + e];
+            vd[(size_t)e * 16] = ((const T *)c.v_one)[new_row + e];
+        }
+    };
+
     if constexpr (BF) {
         // ---- bf16: 16x16x32 MFMAs
         auto body = [&](bool whole, const bf16x8 (&kf)[2][4], bf16x8 (&vf)[HT], unsigned vis) __attribute__((always_inline)) {
@@ -275,6 +290,24 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
                 }
                 body(whole, kf, vf, vis);
             } else {
+                if (u0 == new_unit || u1 == new_unit) {
+                    const int key = (u1 == new_unit ? 16 : 0) + (L & 15);        // of the 32: tile t, row 4a + e is key 8a + 4t + e
+                    const bf16_t *kn = (const bf16_t *)c.k_one + new_row, *vn = (const bf16_t *)c.v_one + new_row;
+#pragma unroll
+                    for (int t = 0; t < 2; ++t)
+                        if (8 * (lq >> 2) + 4 * t + (lq & 3) == key)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                                for (int e = 0; e < 8; ++e) x.k[t][j][e] = kn[32 * j + 8 * kg + e];
+                    if ((key >> 3) == kg)
+#pragma unroll
+                        for (int t = 0; t < HT; ++t)
+#pragma unroll
+                            for (int e = 0; e < 8; ++e)
+                                if (e == (key & 7)) x.v[t][e] = vn[16 * t + lq];
+                    store_new();
+                }
                 body(whole, x.k, x.v, vis);
             }
         };
@@ -410,6 +443,10 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
                 at[t] = piece * 16 * hd;
                 if (KV4 && cache) load_k4(c.kv4.pages + piece * kv4_head_bytes(hd), k);
                 else load_k((const float *)(cache ? c.kv.k_pages : c.k_scr) + at[t], k);
+                if (cache && u[t] == new_unit && lq == (L & 15)) {
+#pragma unroll
+                    for (int j = 0; j < Q4; ++j) k[j] = Q4 * kg + j < hd ? ((const float *)c.k_one)[new_row + Q4 * kg + j] : 0.f;
+                }
                 if (KV4 && cache) at[t] = piece * kv4_head_bytes(hd);
                 s[t] = scores(k);
             }
@@ -421,6 +458,15 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
             for (int t = 0; t < 2; ++t) {
                 if (KV4 && cache) load_v4(c.kv4.pages + at[t], v);
                 else load_v((const float *)(cache ? c.kv.v_pages : c.v_scr) + at[t], v);
+                if (cache && u[t] == new_unit) {
+                    if (((L & 15) >> 2) == kg)
+#pragma unroll
+                        for (int i = 0; i < HT; ++i)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e)
+                                if (e == (L & 3) && HT * lq + i < hd) v[i][e] = ((const float *)c.v_one)[new_row + HT * lq + i];
+                    store_new();
+                }
                 weigh(v, p + 4 * t, vis >> (16 * t));
             }
         }

@@ -419,6 +419,7 @@ struct SpanCall {
     KvView kv;                 // exact pages, or k_pages == nullptr:
     Kv4View kv4;
     const void *k_scr, *v_scr; // the mask rows' tiles
+    const void *k_one, *v_one; // exact pages, one causal row and nothing else: its K/V, which the attention itself caches; else nullptr
     const int32_t *prefix_len;
     RowDesc d;
     int B, n_q;

@@ -1099,7 +1099,10 @@ static tidar_status span_attention(tidar_ctx *ctx, const tidar_kv_cache *kv, con
     call.window = window < kMostPositions ? window : kMostPositions;
     call.sinks = sinks < kMostPositions ? sinks : kMostPositions;
     call.part = (float *)(wsb + l.part);
-    if (kv || d.nm > 0) {
+    if (kv && d.R == 1 && l.plan.tiles == 1 && !l.plan.rows) {        // the one-token step: no launch for its row
+        call.k_one = k_new;
+        call.v_one = v_new;
+    } else if (kv || d.nm > 0) {
         Prof p(ctx, KC_PLACE_KV, st);
         launch_span_place(c.dtype, k_new, v_new, kv ? d.R : d.nm, kv ? d.nc : 0, prefix_len, d, batch, call.kv, wsb + l.k_scr,
                           wsb + l.v_scr, st);
