@@ -619,8 +619,18 @@ SpanPlan plan_span(int dtype, int B, int n_q, int n_kv, int hd, const RowDesc &d
     p.tiles = (F + 15) / 16;
     const long long keys = span_keys(d, d.R, window, sinks, max_prefix);
     const long long wgs = (long long)B * n_kv * p.tiles;
-    const int bound = wgs >= 512 ? 1 : (int)std::min<long long>(64, 1024 / wgs);
-    p.splits = (int)std::max<long long>(1, std::min<long long>(bound, keys / 256));
+    // One round of workgroups, two to a compute unit.  A wave's iteration takes about 0.75 us, the join of the splits 3 and 4 ns
+    // per partial result: the least sum wins.  (us at 1, 2, 4, 8, 16 splits: 32 sequences of 1000 keys in 4 bits 12.6, 15.5, 18.8,
+    // 24.1, 38.3; 8 of 8192 52.9, 32.5, 21.7, 20.3, 24.4; one over an exact window of 4096 43.1, 27.9, 19.2, 14.1, 12.0)
+    const int bound = wgs >= 512 ? 1 : (int)std::min<long long>(64, 512 / wgs);
+    double best = 0.0;
+    for (int s = 1; s <= bound; ++s) {
+        const double t = 0.75 * (double)((keys + 128 * s - 1) / (128 * s)) + (s > 1 ? 3.0 + 0.004 * (double)wgs * s : 0.0);
+        if (s == 1 || t < best) {
+            best = t;
+            p.splits = s;
+        }
+    }
     p.part_floats = bound == 1 ? 0 : (size_t)B * d.R * n_q * bound * (hd + 2);
     return p;
 }
