@@ -7,9 +7,9 @@
 //
 // The walk.  A workgroup takes a tile of 16 query rows of a kv head (the rows of all its query heads, head-major) and walks only the
 // units of 16 keys (cache pages, then mask tiles) that any of its rows sees; any two units make an iteration of 32 keys.  Pages
-// between the sinks and the window are never read, not even their table entries.  The four waves take every fourth iteration,
-// each with its own softmax state, straight from memory into registers (no LDS, no barrier in the loop), and are folded through
-// LDS at the end.  Where the tiles do not fill the chip the walk is cut into key splits, evenly by its real length, and the partial
+// between the sinks and the window are never read, not even their table entries.  The waves take
+// turns with the iterations, each with its own softmax state, straight from memory into registers (no LDS, no barrier in the loop),
+// and are folded through LDS at the end.  Where the tiles do not fill the chip the walk is cut into key splits, evenly by its real length, and the partial
 // results are joined by a second kernel.
 //
 // The softmax.  Scores are formed transposed, S^T[key][q], so that a lane holds one query row's scores of its keys and they are,
@@ -28,15 +28,15 @@
 
 namespace {
 
-// T: bf16 (head_dim 128) or float; KV4: 4-bit pages; HT: head_dim tiles of 16.
-template <class T, bool KV4, int HT>
-__global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
+// T: bf16 (head_dim 128) or float; KV4: 4-bit pages; HT: head_dim tiles of 16; W: waves.
+template <class T, bool KV4, int HT, int W>
+__global__ __launch_bounds__(64 * W, 2) void span_attn_kernel(SpanArgs a) {
     constexpr bool BF = sizeof(T) == 2;
     constexpr int HD = 16 * HT;                          // head_dim, padded to the tiles
     constexpr int Q4 = HD / 4;                           // fp32: head-dim values of a lane's quarter
     constexpr bool QUADS = !BF || KV4;                   // a lane's eight keys: two quads, or a run of eight
-    __shared__ float red[4][16][HD + 4];
-    __shared__ float m_lds[4][16], l_lds[4][16];
+    __shared__ float red[W][16][HD + 4];
+    __shared__ float m_lds[W][16], l_lds[W][16];
     const SpanCall &c = a.c;
     const RowDesc &d = c.d;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -86,8 +86,8 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
     // Page ids of this wave's next 32 iterations, a lane each (0 for a unit that is not there): lane 2 i + t holds unit t's of its
     // i-th iteration from `first` on.  (One scalar load per iteration had to be waited for in each, together with all of LDS.)
     auto load_pages = [&](int first) {
-        const int w = 2 * (first + 4 * (lane >> 1)) + (lane & 1), u = wk.cache_unit(w);
-        int page = first + 4 * (lane >> 1) < it1 && u >= 0 ? pt[u] : 0;
+        const int w = 2 * (first + W * (lane >> 1)) + (lane & 1), u = wk.cache_unit(w);
+        int page = first + W * (lane >> 1) < it1 && u >= 0 ? pt[u] : 0;
         if ((unsigned)page >= (unsigned)n_pages) {
             bad = true;
             page = 0;
@@ -95,9 +95,9 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
         return page;
     };
     int pages = 0, pages_at = 0;
-    auto page_of = [&](int n, int t) { return __builtin_amdgcn_readlane(pages, ((n - pages_at) >> 1) + t); };      // iteration n, unit t
-    auto pages_for = [&](int n) {                        // before iteration n's pages are asked for (n in steps of 4)
-        if (n - pages_at >= 128) {
+    auto page_of = [&](int n, int t) { return __builtin_amdgcn_readlane(pages, 2 * (n - pages_at) / W + t); };      // iteration n, unit t
+    auto pages_for = [&](int n) {                        // before iteration n's pages are asked for (n in steps of W)
+        if (n - pages_at >= 32 * W) {
             pages = load_pages(n);
             pages_at = n;
         }
@@ -315,15 +315,15 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
         int n = it0 + wave;
         if (n < end1) {
             Raw x0 = fetch(n), x1;
-            if (AHEAD == 2 && n + 4 < end1) x1 = fetch(n + 4);
-            for (; n < end1; n += 4) {
+            if (AHEAD == 2 && n + W < end1) x1 = fetch(n + W);
+            for (; n < end1; n += W) {
                 Raw now = x0;
                 if constexpr (AHEAD == 2) x0 = x1;
-                if (n + 4 * AHEAD < end1) (AHEAD == 2 ? x1 : x0) = fetch(n + 4 * AHEAD);
+                if (n + W * AHEAD < end1) (AHEAD == 2 ? x1 : x0) = fetch(n + W * AHEAD);
                 block(n, now);
             }
         }
-        for (; n < it1; n += 4) {
+        for (; n < it1; n += W) {
             const int w = 2 * (n - wk.n1), u0 = wk.mask_unit(w), u1 = wk.mask_unit(w + 1);
             bf16x8 kf[2][4], vf[HT];
             load_exact((const bf16_t *)c.k_scr + mask_tile(u0), (const bf16_t *)c.k_scr + mask_tile(u1),
@@ -429,7 +429,7 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
 #pragma unroll
                 for (int t = 0; t < HT; ++t) acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(v[t][e], p[e], acc[t], 0, 0, 0);
         };
-        for (int n = it0 + wave; n < it1; n += 4) {
+        for (int n = it0 + wave; n < it1; n += W) {
             const bool cache = n < wk.n1;
             const int w = cache ? 2 * n : 2 * (n - wk.n1);
             const int u[2] = {cache ? wk.cache_unit(w) : wk.mask_unit(w), cache ? wk.cache_unit(w + 1) : wk.mask_unit(w + 1)};
@@ -472,7 +472,7 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
         }
     }
 
-    // ---- fold the four waves
+    // ---- fold the waves
     float l = l_run;
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
@@ -492,17 +492,17 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
             red[wave][lq][(BF && !KV4) ? 16 * t + i : HT * i + t] = acc[t][e];
         }
     __syncthreads();
-    constexpr int PER = HD / 16;                         // values of a thread
-    const int oq = tid >> 4, od = (tid & 15) * PER, of = tile * 16 + oq;
+    constexpr int LANES = 4 * W, PER = HD / LANES;       // a row's threads, and the values of each
+    const int oq = tid / LANES, od = (tid % LANES) * PER, of = tile * 16 + oq;
     if (of >= F) return;
     float m = m_lds[0][oq];
 #pragma unroll
-    for (int w = 1; w < 4; ++w) m = fmaxf(m, m_lds[w][oq]);
+    for (int w = 1; w < W; ++w) m = fmaxf(m, m_lds[w][oq]);
     float sum = 0.f, o[PER];
 #pragma unroll
     for (int e = 0; e < PER; ++e) o[e] = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
+    for (int w = 0; w < W; ++w) {
         const float mw = m_lds[w][oq];
         if (mw == -INFINITY) continue;                   // saw nothing
         const float wgt = mw == m ? 1.f : __builtin_amdgcn_exp2f(mw - m);
@@ -516,7 +516,7 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
         const size_t at = orh * a.splits + split;
         for (int e = 0; e < PER; ++e)
             if (od + e < hd) a.opart[at * hd + od + e] = o[e];
-        if ((tid & 15) == 0) {
+        if (tid % LANES == 0) {
             a.mpart[at] = m;
             a.lpart[at] = sum;
         }
@@ -524,10 +524,11 @@ __global__ __launch_bounds__(256, 2) void span_attn_kernel(SpanArgs a) {
     }
     T *out = (T *)c.out + orh * hd + od;
     if constexpr (BF) {
-        bf16x8 v;
+        typedef __attribute__((ext_vector_type(PER))) __bf16 bf16_per;
+        bf16_per v;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = (bf16_t)(o[e] / sum);
-        *(bf16x8 *)out = v;
+        for (int e = 0; e < PER; ++e) v[e] = (bf16_t)(o[e] / sum);
+        *(bf16_per *)out = v;
     } else {
 #pragma unroll
         for (int e = 0; e < PER; ++e)
@@ -600,6 +601,9 @@ __global__ __launch_bounds__(64) void span_combine_kernel(const float *__restric
 
 }  // namespace
 
+// Waves of a few-row workgroup.  bf16: eight, so that half as many splits have to be joined (32 sequences of 8192 keys in 4 bits:
+// 50.6 us unsplit, with four waves 59.7 and 52 at best); fp32: four, the registers of head_dim 128 do not fit twice.
+static int span_waves(int dtype) { return dtype == TIDAR_BF16 ? 8 : 4; }
 constexpr int kFewRows = 64;           // rows of a kv head up to which they are taken 16 to a workgroup
 
 // Keys that a workgroup walks whose rows lie within `rows` positions, from the caller's bound on the prefix.
@@ -619,13 +623,14 @@ SpanPlan plan_span(int dtype, int B, int n_q, int n_kv, int hd, const RowDesc &d
     p.tiles = (F + 15) / 16;
     const long long keys = span_keys(d, d.R, window, sinks, max_prefix);
     const long long wgs = (long long)B * n_kv * p.tiles;
-    // One round of workgroups, two to a compute unit.  A wave's iteration takes about 0.75 us, the join of the splits 3 and 4 ns
-    // per partial result: the least sum wins.  (us at 1, 2, 4, 8, 16 splits: 32 sequences of 1000 keys in 4 bits 12.6, 15.5, 18.8,
-    // 24.1, 38.3; 8 of 8192 52.9, 32.5, 21.7, 20.3, 24.4; one over an exact window of 4096 43.1, 27.9, 19.2, 14.1, 12.0)
-    const int bound = wgs >= 512 ? 1 : (int)std::min<long long>(64, 512 / wgs);
+    // One round of workgroups, eight waves to a compute unit.  A wave's iteration takes about 0.75 us, the join of the splits 3 and
+    // 4 ns per partial result: the least sum wins.  (us at 1, 2, 4, 8, 16 splits: 32 sequences of 1000 keys in 4 bits 12.1, 19.5,
+    // 25.8, 37.5, 65.6; 8 of 8192 40.3, 26.5, 19.8, 25.3, 33.9; one over an exact window of 4096 43.5, 30.0, 19.8, 13.3, 11.3)
+    const int waves = span_waves(dtype), slots = 2048 / waves, per_it = 32 * waves;
+    const int bound = wgs >= slots ? 1 : (int)std::min<long long>(64, slots / wgs);
     double best = 0.0;
     for (int s = 1; s <= bound; ++s) {
-        const double t = 0.75 * (double)((keys + 128 * s - 1) / (128 * s)) + (s > 1 ? 3.0 + 0.004 * (double)wgs * s : 0.0);
+        const double t = 0.75 * (double)((keys + per_it * s - 1) / (per_it * s)) + (s > 1 ? 3.0 + 0.004 * (double)wgs * s : 0.0);
         if (s == 1 || t < best) {
             best = t;
             p.splits = s;
@@ -660,18 +665,18 @@ void launch_span_attention(int dtype, const SpanCall &c, const SpanPlan &p, hipS
     const bool four = c.kv.k_pages == nullptr;
     const int n_kv = four ? c.kv4.n_kv : c.kv.n_kv, hd = four ? c.kv4.hd : c.kv.hd;
     const dim3 grid(c.B * n_kv * p.tiles, p.splits);
-    auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(a); };
+    auto go = [&](auto kernel) { kernel<<<grid, 64 * span_waves(dtype), 0, st>>>(a); };
     if (dtype == TIDAR_BF16) {
-        if (four) go(span_attn_kernel<bf16_t, true, 8>);
-        else go(span_attn_kernel<bf16_t, false, 8>);
+        if (four) go(span_attn_kernel<bf16_t, true, 8, 8>);
+        else go(span_attn_kernel<bf16_t, false, 8, 8>);
     } else if (four) {
-        if (hd <= 32) go(span_attn_kernel<float, true, 2>);
-        else if (hd <= 64) go(span_attn_kernel<float, true, 4>);
-        else go(span_attn_kernel<float, true, 8>);
+        if (hd <= 32) go(span_attn_kernel<float, true, 2, 4>);
+        else if (hd <= 64) go(span_attn_kernel<float, true, 4, 4>);
+        else go(span_attn_kernel<float, true, 8, 4>);
     } else {
-        if (hd <= 32) go(span_attn_kernel<float, false, 2>);
-        else if (hd <= 64) go(span_attn_kernel<float, false, 4>);
-        else go(span_attn_kernel<float, false, 8>);
+        if (hd <= 32) go(span_attn_kernel<float, false, 2, 4>);
+        else if (hd <= 64) go(span_attn_kernel<float, false, 4, 4>);
+        else go(span_attn_kernel<float, false, 8, 4>);
     }
 }
 
