@@ -649,10 +649,12 @@ static SpanArgs span_args(const SpanCall &c, const SpanPlan &p) {
     a.splits = p.splits;
     a.span_rows = p.span_rows;
     a.whole = p.whole;
+    a.per = p.per;
     const size_t rows = p.rows ? (size_t)(c.B * n_kv * p.tiles - p.whole) * p.splits * 128 : (size_t)c.B * c.d.R * c.n_q * p.splits;
     a.opart = c.part;
     a.mpart = c.part + rows * hd;
     a.lpart = a.mpart + rows;
+    a.pieces = (int *)(a.lpart + rows);
     return a;
 }
 

@@ -10,10 +10,11 @@
 // [unit][key half][position] 16-byte pieces, where position p is head-dim value p (exact pages) or 8 (p % 16) + p / 16 (4-bit
 // pages: a wave's stores are contiguous then, and a lane's results are runs of eight values).
 //
-// Two workgroups share a compute unit, 512 run at a time.  As many whole ones as make full rounds go first; the walk of the rest,
-// whose round would leave most of the chip idle, is cut into key splits (SpanPlan), and only their partial results are written
-// and joined.
+// Two workgroups share a compute unit, 512 run at a time.  As many whole ones as make full rounds go first; the walks of the rest,
+// whose round would leave most of the chip idle, are cut into pieces of equal length (SpanPlan), and only their partial results are
+// written and joined.
 #include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 #include "lds_dma.h"
@@ -42,12 +43,46 @@ __device__ inline Place place_of(const SpanArgs &a, int n_kv, int item) {
         chunk = item % a.tiles;
     }
     const int per_span = (a.span_rows + ROWS - 1) / ROWS, span = chunk / per_span;
+    // every other span backwards: the chunks of causal rows grow, and with them in one order an XCD got the long ones of all heads
+    const int at = chunk - span * per_span, spans = a.tiles / per_span;
     Place p;
     p.b = grp / n_kv;
     p.g = grp - p.b * n_kv;
-    p.f0 = span * a.span_rows + (chunk - span * per_span) * ROWS;
+    p.f0 = span * a.span_rows + ((grp * spans + span) & 1 ? per_span - 1 - at : at) * ROWS;
     p.f1 = min(min(p.f0 + ROWS, (span + 1) * a.span_rows), F);
     return p;
+}
+
+// The bounds that a walk needs (lo0, hi1, sk1, m0, m1) of rows [r0, r1) of a query head, and of a workgroup's rows.
+__device__ inline RowBounds head_bounds(const RowDesc &d, int L, int r0, int r1, int window, int sinks) {
+    int first = 0x7fffffff, hi = 0, m0 = 0x7fffffff, m1 = 0;             // first: the least position of a row
+    if (r0 < d.nc) {
+        first = L + r0;
+        hi = L + min(r1, d.nc);
+    }
+    if (r1 > d.nc) {
+        const int a = max(r0, d.nc) - d.nc, j0 = a / d.bl, j1 = (r1 - 1 - d.nc) / d.bl;
+        first = min(first, L + d.cond0 + j0 * d.cstride + a - j0 * d.bl);
+        if (j1 > j0) first = min(first, L + d.cond0 + (j0 + 1) * d.cstride);
+        hi = max(hi, L + d.cond0 + j1 * d.cstride);
+        m0 = j0 * d.bl;
+        m1 = min((j1 + 1) * d.bl, d.nm);
+    }
+    return {window > 0 ? max(0, first - window + 1) : 0, 0, 0, hi, 0, window > 0 ? min(sinks, hi) : 0, m0, m1};
+}
+__device__ inline Walk walk_at(const SpanArgs &a, const Place &p, int L) {
+    const RowDesc &d = a.c.d;
+    const int h0 = p.f0 / d.R, h1 = (p.f1 - 1) / d.R, ra = p.f0 - h0 * d.R, rb = p.f1 - h1 * d.R;
+    const int w = a.c.window, t = a.c.sinks;
+    return walk_of(h0 == h1 ? head_bounds(d, L, ra, rb, w, t)
+                            : h1 == h0 + 1 ? join(head_bounds(d, L, ra, d.R, w, t), head_bounds(d, L, 0, rb, w, t))
+                                           : head_bounds(d, L, 0, d.R, w, t), w);
+}
+__device__ inline bool length_of(const SpanArgs &a, int b, int pps, int &L) {
+    const int x = a.c.prefix_len[a.c.d.seq_base + b];
+    const bool fits = x >= 0 && (long long)x + a.c.d.nc <= (long long)pps * 16;
+    L = fits ? x : 0;
+    return fits;
 }
 
 // A lane's results: 16 pieces of four values (t, h) of its row, normalised, into the output.  KV4: value e of piece (t, h) is
@@ -77,7 +112,7 @@ __device__ inline void store_row(bf16_t *out, const f32x4 (&x)[4][4], float inv,
                                                                       (bf16_t)(x[t][h][2] * inv), (bf16_t)(x[t][h][3] * inv)};
     }
 }
-// Where the partial results of tile `wave` of a split are: 16 pieces as they lie in the registers, a store being one contiguous KiB.
+// Where the partial results of tile `wave` of piece `part` are: 16 pieces as they lie in the registers, a store being one contiguous KiB.
 __device__ inline f32x4 *partial_of(const SpanArgs &a, int part, int wave) {
     return (f32x4 *)a.opart + ((size_t)part * 4 + wave) * 16 * 64;
 }
@@ -86,7 +121,6 @@ template <bool KV4>
 __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
     __shared__ __attribute__((aligned(16))) bf16_t k_lds[RING][TILE];
     __shared__ __attribute__((aligned(16))) bf16_t v_lds[RING][TILE];
-    __shared__ RowBounds wave_rows[4];
     __shared__ int bad_lds;
     const SpanCall &c = a.c;
     const RowDesc &d = c.d;
@@ -94,14 +128,60 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
     const int lq = lane & 31, lh = lane >> 5;
     const int n_kv = KV4 ? c.kv4.n_kv : c.kv.n_kv;
     const int pps = KV4 ? c.kv4.pages_per_seq : c.kv.pages_per_seq, n_pages = KV4 ? c.kv4.n_pages : c.kv.n_pages;
-    const int cut = (int)blockIdx.x - a.whole, rest = c.B * n_kv * a.tiles - a.whole;          // cut >= 0: one of the key splits
-    const int splits = cut < 0 ? 1 : a.splits, split = cut < 0 ? 0 : cut / rest;
-    const int item = cut < 0 ? (int)blockIdx.x : a.whole + cut % rest;
+    const int cut = (int)blockIdx.x - a.whole;           // >= 0: a piece of a walk
+    int item = blockIdx.x, split = 0, splits = 1;
+    if (cut >= 0) {
+        // Piece `cut` of the walks that are cut, numbered walk by walk; each has as many as it is long (a table of their first
+        // pieces, made by every workgroup for itself: a launch with empty pieces between the others left a quarter of the
+        // compute units without work while others had three).  Two of at most 511 walks to a thread.
+        int *first = reinterpret_cast<int *>(&k_lds[0][0]), *sums = first + 514;
+        const int rest = c.B * n_kv * a.tiles - a.whole;
+        int n[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            n[k] = 0;
+            if (2 * tid + k < rest) {
+                const Place p = place_of(a, n_kv, a.whole + 2 * tid + k);
+                int L;
+                n[k] = 1;
+                if (length_of(a, p.b, pps, L)) {
+                    const Walk w = walk_at(a, p, L);
+                    n[k] = max(1, min(a.splits, (w.n1 + w.n2 + a.per - 1) / a.per));
+                }
+            }
+        }
+        int sum = n[0] + n[1];
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int x = __shfl_up(sum, o);
+            if (lane >= o) sum += x;
+        }
+        if (lane == 63) sums[wave] = sum;
+        __syncthreads();
+        for (int w = 0; w < wave; ++w) sum += sums[w];
+        first[2 * tid] = sum - n[0] - n[1];
+        first[2 * tid + 1] = sum - n[1];
+        if (tid == 255) first[512] = sum;
+        __syncthreads();
+        if (cut >= first[512]) return;                   // fewer pieces than the bound allows for (whole workgroup)
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+            if (first[2 * tid + k] <= cut && cut < first[2 * tid + k] + n[k]) sums[4] = 2 * tid + k;
+        __syncthreads();
+        item = __builtin_amdgcn_readfirstlane(sums[4]);
+        split = __builtin_amdgcn_readfirstlane(cut - first[item]);
+        splits = __builtin_amdgcn_readfirstlane(first[item + 1] - first[item]);
+        if (split == 0 && tid == 0) {                    // for the join
+            a.pieces[2 * item] = cut;
+            a.pieces[2 * item + 1] = splits;
+        }
+        item += a.whole;
+        __syncthreads();                                 // the table's place is a tile's
+    }
     const Place pl = place_of(a, n_kv, item);
     const int b = pl.b, g = pl.g;
-    const int L_raw = c.prefix_len[d.seq_base + b];
-    const bool fits = L_raw >= 0 && (long long)L_raw + d.nc <= (long long)pps * 16;
-    const int L = fits ? L_raw : 0;
+    int L;
+    const bool fits = length_of(a, b, pps, L);
     const int f = pl.f0 + wave * 32 + lq;
     const bool here = pl.f0 + wave * 32 < pl.f1, row = f < pl.f1;        // (here: wave-uniform)
     const int hq = row ? f / d.R : 0, r = row ? f - hq * d.R : 0;
@@ -109,15 +189,10 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
     RowSpan rs = row_span(d, r, L, c.window, c.sinks);
     const RowBounds rb = wave_bounds<32>(bounds_of(rs, row));
     if (!row) rs = RowSpan{};
-    if (lane == 0) wave_rows[wave] = rb;
     if (tid == 0) bad_lds = 0;
-    __syncthreads();
-    const RowBounds all = join(join(wave_rows[0], wave_rows[1]), join(wave_rows[2], wave_rows[3]));
-    auto uni = [](int v) { return __builtin_amdgcn_readfirstlane(v); };
-    const Walk wk = walk_of({uni(all.lo0), uni(all.lo1), uni(all.hi0), uni(all.hi1), uni(all.sk0), uni(all.sk1), uni(all.m0),
-                             uni(all.m1)}, c.window);
-    const int n_it = fits ? wk.n1 + wk.n2 : 0, per = (n_it + splits - 1) / splits;
-    const int it0 = min(n_it, split * per), n_seq = min(n_it, it0 + per) - it0;
+    const Walk wk = walk_at(a, pl, L);
+    const int n_it = fits ? wk.n1 + wk.n2 : 0, it0 = min(n_it, split * a.per);
+    const int n_seq = (split == splits - 1 ? n_it : min(n_it, it0 + a.per)) - it0;
     const int32_t *pt = (KV4 ? c.kv4.page_table : c.kv.page_table) + (size_t)(d.seq_base + b) * pps;
     const int n_mt = (d.nm + 15) >> 4;
     bool bad = !fits;
@@ -412,77 +487,88 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
         if (row) store_row<KV4>((bf16_t *)c.out + orh * HD, x, 1.f / l, lh);
         return;
     }
-    const int part = (item - a.whole) * a.splits + split;
-    f32x4 *op = partial_of(a, part, wave) + lane;
+    f32x4 *op = partial_of(a, cut, wave) + lane;
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int h = 0; h < 4; ++h) op[(4 * t + h) * 64] = x[t][h];
     if (lh == 0) {
-        a.mpart[(size_t)part * ROWS + wave * 32 + lq] = m_run;
-        a.lpart[(size_t)part * ROWS + wave * 32 + lq] = l;
+        a.mpart[(size_t)cut * ROWS + wave * 32 + lq] = m_run;
+        a.lpart[(size_t)cut * ROWS + wave * 32 + lq] = l;
     }
 }
 
-// out = sum_s w_s O_s / sum_s w_s l_s, w_s = 2^(m_s - max m), of the workgroups that were cut: a wave takes a quarter of the results
-// of a tile of 32 rows.
+// out = sum_s w_s O_s / sum_s w_s l_s, w_s = 2^(m_s - max m), of the workgroups that were cut.  A wave takes half of the
+// results of a tile of 32 rows: pieces (t, h) and (t, h + 2) of all t, whole runs of eight values with 4-bit pages.
 template <bool KV4>
-__global__ __launch_bounds__(256) void span_rows_join_kernel(SpanArgs a) {
+__global__ __launch_bounds__(128) void span_rows_join_kernel(SpanArgs a) {
     const SpanCall &c = a.c;
     const RowDesc &d = c.d;
-    const int lane = threadIdx.x & 63, lq = lane & 31, lh = lane >> 5, t = threadIdx.x >> 6, wave = blockIdx.x & 3;
+    const int lane = threadIdx.x & 63, lq = lane & 31, lh = lane >> 5, half = threadIdx.x >> 6, wave = blockIdx.x & 3;
     const int tail = blockIdx.x >> 2, n_kv = KV4 ? c.kv4.n_kv : c.kv.n_kv;
     const Place pl = place_of(a, n_kv, a.whole + tail);
     const int f = pl.f0 + wave * 32 + lq;
     if (pl.f0 + wave * 32 >= pl.f1) return;
-    const int S = a.splits, part = tail * S;
+    const int part = a.pieces[2 * tail], S = a.pieces[2 * tail + 1];
     const float *mp = a.mpart + (size_t)part * ROWS + wave * 32 + lq, *lp = a.lpart + (size_t)part * ROWS + wave * 32 + lq;
     float m = -INFINITY;
 #pragma unroll 8
     for (int s = 0; s < S; ++s) m = fmaxf(m, mp[(size_t)s * ROWS]);
-    f32x4 num[4];
+    f32x4 num[4][2];
     float den = 0.f;
 #pragma unroll
-    for (int h = 0; h < 4; ++h) num[h] = (f32x4){0.f, 0.f, 0.f, 0.f};
-    for (int s0 = 0; s0 < S; s0 += 4) {
-        f32x4 x[4][4];
-        float ms[4], ls[4];
+    for (int t = 0; t < 4; ++t) num[t][0] = num[t][1] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    for (int s0 = 0; s0 < S; s0 += 2) {
+        f32x4 x[2][4][2];
+        float ms[2], ls[2];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < 2; ++j) {
             const int s = min(s0 + j, S - 1);
-            const f32x4 *op = partial_of(a, part + s, wave) + 4 * t * 64 + lane;
-#pragma unroll
-            for (int h = 0; h < 4; ++h) x[j][h] = op[h * 64];
             ms[j] = s0 + j < S ? mp[(size_t)s * ROWS] : -INFINITY;
             ls[j] = lp[(size_t)s * ROWS];
+            const f32x4 *op = partial_of(a, part + s, wave) + lane;
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) x[j][t][i] = op[(4 * t + half + 2 * i) * 64];
         }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
+        for (int j = 0; j < 2; ++j) {
             if (ms[j] == -INFINITY) continue;            // saw nothing
             const float w = ms[j] == m ? 1.f : __builtin_amdgcn_exp2f(ms[j] - m);
             den += w * ls[j];
 #pragma unroll
-            for (int h = 0; h < 4; ++h)
+            for (int t = 0; t < 4; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) num[h][e] += w * x[j][h][e];
+                for (int i = 0; i < 2; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) num[t][i][e] += w * x[j][t][i][e];
         }
     }
     if (f >= pl.f1) return;
     const float inv = 1.f / den;
     const int hq = f / d.R, r = f - hq * d.R;
     bf16_t *out = (bf16_t *)c.out + (((size_t)pl.b * d.R + r) * c.n_q + pl.g * a.group + hq) * HD;
+    if constexpr (KV4) {
 #pragma unroll
-    for (int h = 0; h < 4; ++h) {
-        if constexpr (KV4) {
-            if (h < 2)
+        for (int e = 0; e < 4; ++e) {
+            bf16x8 o;
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    *(bf16x2 *)(out + 8 * (8 * h + 4 * lh + e) + 2 * t) = (bf16x2){(bf16_t)(num[h][e] * inv), (bf16_t)(num[h + 2][e] * inv)};
-        } else {
-            typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
-            *(bf16x4 *)(out + 32 * t + 8 * h + 4 * lh) =
-                (bf16x4){(bf16_t)(num[h][0] * inv), (bf16_t)(num[h][1] * inv), (bf16_t)(num[h][2] * inv), (bf16_t)(num[h][3] * inv)};
+            for (int t = 0; t < 4; ++t) {
+                o[2 * t] = (bf16_t)(num[t][0][e] * inv);
+                o[2 * t + 1] = (bf16_t)(num[t][1][e] * inv);
+            }
+            *(bf16x8 *)(out + 8 * (8 * half + 4 * lh + e)) = o;
         }
+    } else {
+        typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                *(bf16x4 *)(out + 32 * t + 8 * (half + 2 * i) + 4 * lh) =
+                    (bf16x4){(bf16_t)(num[t][i][0] * inv), (bf16_t)(num[t][i][1] * inv), (bf16_t)(num[t][i][2] * inv),
+                             (bf16_t)(num[t][i][3] * inv)};
     }
 }
 
@@ -490,30 +576,42 @@ int groups_of(const SpanArgs &a) { return a.c.B * (a.c.kv.k_pages ? a.c.kv.n_kv 
 
 }  // namespace
 
-// Whole workgroups first, then the key splits of the rest: of every round but the last 512 workgroups, two to a compute unit, run at a
-// time.  The rest (fewer than 512) is cut into the number of splits that takes the least time, in iterations of about a microsecond
-// with two workgroups to a unit: eight for a workgroup's prologue, twelve more where its partial results (66 KB) go out and come
-// back; no more than 1024 workgroups and one per four iterations.  That bound sizes the workspace, which then depends
-// on the rows alone.
+// Whole workgroups first, then the pieces of the rest: of every round but the last 512 workgroups, two to a compute unit, run at a
+// time.  The rest (fewer than 512) is cut into pieces of equal length, at most `splits` of each, as many as take the least time.
+// An iteration takes 1.2 us with two workgroups on every unit and 0.8 with one; a workgroup has a prologue of about eight iterations,
+// and twelve more where its partial results (66 KB) go out and come back.  No more than 1024 workgroups and one per four
+// iterations: that bound sizes the workspace, which then depends on the rows alone.
 void plan_span_rows(int B, int n_kv, int group, const RowDesc &d, int window, int sinks, int max_prefix, SpanPlan *p) {
     const int F = group * d.R;
     // rows of one head see one run of keys where they are many: chunks that run over the end of a head would walk all of them
     p->span_rows = d.nc >= ROWS ? d.R : F;
-    p->tiles = F / p->span_rows * ((p->span_rows + ROWS - 1) / ROWS);
+    const int per_span = (p->span_rows + ROWS - 1) / ROWS;
+    p->tiles = F / p->span_rows * per_span;
     const int items = B * n_kv * p->tiles, rest = items % 512;
     const int most = rest ? std::min(64, 1024 / rest) : 1;
     const int iters = (int)((span_keys(d, p->span_rows == F ? d.R : ROWS, window, sinks, max_prefix) + 31) / 32);
+    // workgroups that have something to do: without a window the causal rows of a chunk see what is before them only
+    auto busy = [&](int s, int per) {
+        if (s == 1 || window > 0 || p->span_rows == F) return (double)rest * s;
+        double n = 0.0;
+        for (int k = 1; k <= per_span; ++k) n += ((max_prefix + std::min(ROWS * k, d.R) + 31) / 32 + per - 1) / per;
+        return n / per_span * rest;
+    };
     p->splits = 1;
+    p->per = 1 << 30;
     double best = 0.0;
     for (int s = 1; s <= most && (s == 1 || 4 * s <= iters); ++s) {
-        const double t = (double)((rest * s + 511) / 512) * ((iters + s - 1) / s + (s == 1 ? 8 : 20));
+        const int per = (iters + s - 1) / s;
+        const double rounds = std::ceil(busy(s, per) / 256.0);            // of one workgroup per unit
+        const double full = std::floor(rounds / 2.0), t = (1.2 * full + 0.8 * (rounds - 2.0 * full)) * (per + (s == 1 ? 8 : 20));
         if (s == 1 || t < 0.97 * best) {
             best = t;
             p->splits = s;
+            p->per = s == 1 ? 1 << 30 : per;
         }
     }
     p->whole = p->splits == 1 ? items : items - rest;
-    p->part_floats = most > 1 ? (size_t)rest * most * ROWS * (HD + 2) : 0;
+    p->part_floats = most > 1 ? (size_t)rest * (most * ROWS * (HD + 2) + 2) : 0;
 }
 
 void launch_span_rows(const SpanArgs &a, hipStream_t st) {
@@ -524,6 +622,6 @@ void launch_span_rows(const SpanArgs &a, hipStream_t st) {
 
 void launch_span_rows_join(const SpanArgs &a, hipStream_t st) {
     const int tail = groups_of(a) * a.tiles - a.whole;
-    if (a.c.kv.k_pages) span_rows_join_kernel<false><<<tail * 4, 256, 0, st>>>(a);
-    else span_rows_join_kernel<true><<<tail * 4, 256, 0, st>>>(a);
+    if (a.c.kv.k_pages) span_rows_join_kernel<false><<<tail * 4, 128, 0, st>>>(a);
+    else span_rows_join_kernel<true><<<tail * 4, 128, 0, st>>>(a);
 }

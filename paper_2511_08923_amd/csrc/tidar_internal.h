@@ -430,14 +430,16 @@ struct SpanPlan {
     bool rows;                 // many rows (kernels_span_rows.hip): 128 to a workgroup, else 16
     int span_rows;             // workgroups of many rows do not run over a multiple of this: a query head's rows, or all of them
     int whole;                 // and so many of them walk all of their keys, the others are cut into splits
+    int per;                   // of so many iterations (of 32 keys) each
     int tiles;                 // workgroups per kv head and key split
     int splits;                // of the keys
     size_t part_floats;
 };
 struct SpanArgs {
     SpanCall c;
-    int group, tiles, splits, span_rows, whole;
+    int group, tiles, splits, span_rows, whole, per;
     float *opart, *mpart, *lpart;
+    int *pieces;               // many rows: first piece and number of pieces of the walks that are cut
 };
 long long span_keys(const RowDesc &d, int rows, int window, int sinks, int max_prefix);
 void plan_span_rows(int B, int n_kv, int group, const RowDesc &d, int window, int sinks, int max_prefix, SpanPlan *p);
