@@ -338,6 +338,10 @@ __global__ __launch_bounds__(256) void span_place_kernel(const T *__restrict__ k
             vt[s0 + r][e] = v_new[src + r * stride + e];
         }
     }
+    if (unit >= n_cache_units) {                          // behind the mask rows: zeros, the attention need not look closer
+        for (int i = tid; i < (16 - n) * hd; i += 256) vt[n + i / hd][i % hd] = (T)0.f;
+        n = 16;
+    }
     __syncthreads();
     for (int i = tid; i < hd * (16 / E); i += 256) {      // a run of E tokens of one element
         const int e = i / (16 / E), s = (i - e * (16 / E)) * E;

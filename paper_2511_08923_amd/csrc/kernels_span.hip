@@ -184,14 +184,22 @@ __global__ __launch_bounds__(64 * W, 2) void span_attn_kernel(SpanArgs a) {
                 }
                 if (__builtin_expect(__any(odd != 0), 0)) {
                     // taken out of the fragments, and added for the rows that see them, key by key through the wave's share of
-                    // LDS (rare, and written to need few registers)
+                    // LDS (rare, and written to need few registers; what lies in slots that no row sees costs the first step only)
                     unsigned short *v = reinterpret_cast<unsigned short *>(&red[wave][0][0]);
+                    unsigned mine = 0, keys = 0;
+#pragma unroll
+                    for (int t = 0; t < HT; ++t) mine |= nonfinite8(vf[t]);
+#pragma unroll
+                    for (int o = 1; o < 16; o <<= 1) mine |= __shfl_xor(mine, o);
+#pragma unroll
+                    for (int q8 = 0; q8 < 4; ++q8) keys |= __builtin_amdgcn_readlane(mine, 16 * q8) << (8 * q8);
 #pragma unroll
                     for (int t = 0; t < HT; ++t) *(bf16x8 *)(v + (16 * t + lq) * 32 + 8 * kg) = vf[t];
 #pragma unroll 1
                     for (int i = 0; i < 32; ++i) {       // slot i % 8 of the lanes of quarter i / 8
                         const int q8 = i >> 3, e = i & 7;
                         const bool seen = (vis >> (QUADS ? 16 * (e >> 2) + 4 * q8 + (e & 3) : i)) & 1u;
+                        if (!((keys >> i) & 1u) || !__any(seen)) continue;
 #pragma unroll
                         for (int t = 0; t < HT; ++t)
 #pragma unroll

@@ -346,7 +346,8 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
             for (int u = 0; u < 2; ++u) vf[t][u] = *(const bf16x8 *)(p + (((u * 2 + lh) * 128 + 32 * t + lq) << 4));
     };
     // V^T values that are not finite, of a block that not every row sees whole: taken out of the fragments, and added for the
-    // rows that see them, key by key from LDS (rare, and written to need few registers)
+    // rows that see them, key by key from LDS (rare, and written to need few registers; what lies in slots that no row
+    // sees, unset memory perhaps, costs the first step only)
     auto set_aside = [&](int m, bf16x8 (&vf)[4][2], unsigned vis) __attribute__((always_inline)) {
         unsigned odd = 0;
 #pragma unroll
@@ -358,8 +359,18 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
             }
         if (__builtin_expect(__any(odd != 0), 0)) {
             const unsigned short *v = reinterpret_cast<const unsigned short *>(&v_lds[m & (RING - 1)][0]);
+            unsigned keys = 0;                           // this lane's: bit 8 u + e
+#pragma unroll
+            for (int t = 0; t < 4; ++t)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) keys |= nonfinite8(vf[t][u]) << (8 * u);
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) keys |= __shfl_xor(keys, o);
+            const unsigned other = __shfl_xor(keys, 32), lo = lh ? other : keys, hi = lh ? keys : other;
+            keys = __builtin_amdgcn_readfirstlane((lo & 0xffu) | ((hi & 0xffu) << 8) | ((lo & 0xff00u) << 8) | ((hi & 0xff00u) << 16));
 #pragma unroll 1
             for (int key = 0; key < 32; ++key) {
+                if (!((keys >> key) & 1u) || !__any((vis >> key) & 1u)) continue;
                 const unsigned short *p = v + (key >> 3) * 1024 + (key & 7) + 32 * lh;
 #pragma unroll
                 for (int t = 0; t < 4; ++t)

@@ -100,6 +100,16 @@ __device__ inline unsigned mask_bits(const RowSpan &s, int u) {
 
 // of two bf16 values: bits where one is not finite; and zeros in the places of those
 __device__ inline unsigned nonfinite2(unsigned x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+__device__ inline unsigned nonfinite8(bf16x8 v) {        // the same as bits 0 .. 7 of eight values
+    const u32x4 w = __builtin_bit_cast(u32x4, v);
+    unsigned m = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const unsigned x = nonfinite2(w[i]);
+        m |= (((x >> 15) & 1u) | ((x >> 30) & 2u)) << (2 * i);
+    }
+    return m;
+}
 __device__ inline bf16x8 finite_only(bf16x8 v) {
     u32x4 w = __builtin_bit_cast(u32x4, v);
 #pragma unroll
