@@ -612,7 +612,14 @@ __global__ __launch_bounds__(64) void span_combine_kernel(const float *__restric
 // Waves of a few-row workgroup.  bf16: eight, so that half as many splits have to be joined (32 sequences of 8192 keys in 4 bits:
 // 50.6 us unsplit, with four waves 59.7 and 52 at best); fp32: four, the registers of head_dim 128 do not fit twice.
 static int span_waves(int dtype) { return dtype == TIDAR_BF16 ? 8 : 4; }
-constexpr int kFewRows = 64;           // rows of a kv head up to which they are taken 16 to a workgroup
+static int most_splits(int dtype, long long wgs) {
+    const int slots = 2048 / span_waves(dtype);
+    return wgs >= slots ? 1 : (int)std::min<long long>(64, slots / wgs);
+}
+static size_t few_part_floats(int dtype, long long wgs, int hd) {
+    const int s = most_splits(dtype, wgs);
+    return s == 1 ? 0 : (size_t)(wgs * 16 * s) * (hd + 2);
+}
 
 // Keys that a workgroup walks whose rows lie within `rows` positions, from the caller's bound on the prefix.
 long long span_keys(const RowDesc &d, int rows, int window, int sinks, int max_prefix) {
@@ -620,22 +627,38 @@ long long span_keys(const RowDesc &d, int rows, int window, int sinks, int max_p
     return window > 0 ? std::min(all, (long long)window + sinks + rows) : all;
 }
 
-SpanPlan plan_span(int dtype, int B, int n_q, int n_kv, int hd, const RowDesc &d, int window, int sinks, int max_prefix) {
+// 16 rows to a workgroup or 128: a wave that takes 16 rows starts and ends sooner, one that takes 32 reads its keys for twice as
+// many and shares them with three others.  What decides is the work in 16 rows by 32 keys, all sequences and heads together, and
+// that the rows fill enough of a workgroup's 128.  us with 16 and with 128 rows:
+//   4-bit pages   8 sequences of 1000 keys and 288 rows (39 k): 51.0, 40.7;  1 of 8000 and 288 (36 k): 43.7, 41.8;
+//                 8 of 1000 and 168 (23 k): 34.4, 36.7;  1 of 8000 and 432 (14 k): 22.2, 36.1;  8 of 8000 and 48 (48 k): 46.0, 57.0
+//   exact pages   a window of 2000, 8 sequences and 72 rows (5.0 k): 27.9, 25.8;  24 (8.1 k): 28.6, 28.3;  36 (12 k): 35.8, 30.9;
+//                 1 and 432 (3.5 k): 19.5, 27.5;  1 and 288 (9.4 k): 28.0, 26.3;  8 and 288 (75 k): 118.6, 57.6
+static bool many_rows(int dtype, bool four, int F, long long wgs, long long keys) {
+    if (dtype != TIDAR_BF16) return false;
+    const long long work = wgs * ((keys + 31) / 32);
+    return four ? F > 64 && work > 36000 : F > 32 && work > 7000;
+}
+
+// The partial results' memory does not depend on that choice, nor on the keys: a caller's bound on the prefixes may differ from the
+// one that it asked the workspace's size for.
+SpanPlan plan_span(int dtype, bool four, int B, int n_q, int n_kv, int hd, const RowDesc &d, int window, int sinks, int max_prefix) {
     SpanPlan p = {};
     const int F = n_q / n_kv * d.R;
-    p.rows = dtype == TIDAR_BF16 && F > kFewRows;
+    const long long keys = span_keys(d, d.R, window, sinks, max_prefix);
+    const long long wgs = (long long)B * n_kv * ((F + 15) / 16);
+    if (dtype == TIDAR_BF16 && F > 32) plan_span_rows(B, n_kv, n_q / n_kv, d, window, sinks, max_prefix, &p);
+    p.rows = many_rows(dtype, four, F, wgs, keys);
     if (p.rows) {
-        plan_span_rows(B, n_kv, n_q / n_kv, d, window, sinks, max_prefix, &p);
+        p.part_floats = std::max(p.part_floats, few_part_floats(dtype, wgs, hd));
         return p;
     }
     p.tiles = (F + 15) / 16;
-    const long long keys = span_keys(d, d.R, window, sinks, max_prefix);
-    const long long wgs = (long long)B * n_kv * p.tiles;
     // One round of workgroups, eight waves to a compute unit.  A wave's iteration takes about 0.75 us, the join of the splits 3 and
     // 4 ns per partial result: the least sum wins.  (us at 1, 2, 4, 8, 16 splits: 32 sequences of 1000 keys in 4 bits 12.1, 19.5,
     // 25.8, 37.5, 65.6; 8 of 8192 40.3, 26.5, 19.8, 25.3, 33.9; one over an exact window of 4096 43.5, 30.0, 19.8, 13.3, 11.3)
-    const int waves = span_waves(dtype), slots = 2048 / waves, per_it = 32 * waves;
-    const int bound = wgs >= slots ? 1 : (int)std::min<long long>(64, slots / wgs);
+    const int per_it = 32 * span_waves(dtype), bound = most_splits(dtype, wgs);
+    p.splits = 1;
     double best = 0.0;
     for (int s = 1; s <= bound; ++s) {
         const double t = 0.75 * (double)((keys + per_it * s - 1) / (per_it * s)) + (s > 1 ? 3.0 + 0.004 * (double)wgs * s : 0.0);
@@ -644,7 +667,7 @@ SpanPlan plan_span(int dtype, int B, int n_q, int n_kv, int hd, const RowDesc &d
             p.splits = s;
         }
     }
-    p.part_floats = bound == 1 ? 0 : (size_t)B * d.R * n_q * bound * (hd + 2);
+    p.part_floats = std::max(p.part_floats, few_part_floats(dtype, wgs, hd));
     return p;
 }
 

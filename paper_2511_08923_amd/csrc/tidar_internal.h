@@ -445,6 +445,6 @@ long long span_keys(const RowDesc &d, int rows, int window, int sinks, int max_p
 void plan_span_rows(int B, int n_kv, int group, const RowDesc &d, int window, int sinks, int max_prefix, SpanPlan *p);
 void launch_span_rows(const SpanArgs &a, hipStream_t st);
 void launch_span_rows_join(const SpanArgs &a, hipStream_t st);
-SpanPlan plan_span(int dtype, int B, int n_q, int n_kv, int hd, const RowDesc &d, int window, int sinks, int max_prefix);
+SpanPlan plan_span(int dtype, bool four, int B, int n_q, int n_kv, int hd, const RowDesc &d, int window, int sinks, int max_prefix);
 void launch_span_attention(int dtype, const SpanCall &c, const SpanPlan &p, hipStream_t st);
 void launch_span_combine(int dtype, const SpanCall &c, const SpanPlan &p, hipStream_t st);

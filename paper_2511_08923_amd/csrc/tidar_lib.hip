@@ -628,7 +628,7 @@ bool span_rows(int batch, int32_t n_causal, int32_t n_blocks, int32_t block_len,
     if (n_causal < 1 || n_blocks < 0 || block_len < 1 || block_len > TIDAR_MAX_K || cond0 < 0) return false;
     if (n_blocks > 0 && (int64_t)cond0 + n_blocks - 1 > n_causal) return false;
     const int64_t rows = (int64_t)n_causal + (int64_t)n_blocks * block_len;
-    if (rows * batch * c.n_q_heads > (int64_t)1 << 26) return false;
+    if (rows > (int64_t)1 << 18 || rows * batch * c.n_q_heads > (int64_t)1 << 26) return false;
     d->nc = n_causal;
     d->nb = n_blocks;
     d->bl = block_len;
@@ -644,9 +644,9 @@ struct SpanLayout {
     SpanPlan plan;
     size_t k_scr, v_scr, part, total;
 };
-SpanLayout span_layout(const tidar_config &c, int batch, const RowDesc &d, int window, int sinks, int max_prefix) {
+SpanLayout span_layout(const tidar_config &c, bool four, int batch, const RowDesc &d, int window, int sinks, int max_prefix) {
     SpanLayout l;
-    l.plan = plan_span(c.dtype, batch, c.n_q_heads, c.n_kv_heads, c.head_dim, d, window, sinks, max_prefix);
+    l.plan = plan_span(c.dtype, four, batch, c.n_q_heads, c.n_kv_heads, c.head_dim, d, window, sinks, max_prefix);
     const size_t scr = align_up((size_t)batch * c.n_kv_heads * ((d.nm + 15) / 16) * 16 * c.head_dim * esize(c.dtype));
     l.k_scr = 0;
     l.v_scr = scr;
@@ -1058,7 +1058,7 @@ tidar_status tidar_attention_workspace_bytes(const tidar_ctx *ctx, int32_t batch
     if (!span_rows(batch, n_causal, n_blocks, block_len, 0, ctx->cfg, &d)) return TIDAR_EINVAL;
     size_t most = 0;
     for (int b = 1; b <= batch; ++b) {          // fewer sequences can take more key splits
-        const SpanLayout l = span_layout(ctx->cfg, b, d, 0, 0, max_prefix_len);
+        const SpanLayout l = span_layout(ctx->cfg, false, b, d, 0, 0, max_prefix_len);
         most = l.total > most ? l.total : most;
     }
     *bytes = most;
@@ -1080,7 +1080,7 @@ static tidar_status span_attention(tidar_ctx *ctx, const tidar_kv_cache *kv, con
     if (!span_rows(batch, n_causal, n_blocks, block_len, cond0, c, &d)) return TIDAR_EINVAL;
     const int32_t pps = kv ? kv->pages_per_seq : kv4->pages_per_seq;
     if ((int64_t)max_prefix_len_hint + n_causal > (int64_t)pps * TIDAR_PAGE_SIZE) return TIDAR_ECAPACITY;
-    const SpanLayout l = span_layout(c, batch, d, window, sinks, max_prefix_len_hint);
+    const SpanLayout l = span_layout(c, kv == nullptr, batch, d, window, sinks, max_prefix_len_hint);
     if (l.total > ws_bytes) return TIDAR_ENOMEM;
     hipStream_t st = (hipStream_t)stream;
     char *wsb = (char *)ws;

@@ -84,7 +84,8 @@ def test_attention_refusals(T, ctx, four):
     for bad in (dict(ctx=None), dict(layer=-1), dict(layer=2), dict(batch=0), dict(batch=9), dict(pl=None), dict(q=None),
                 dict(q=P + 2), dict(k=None), dict(v=None), dict(nc=0), dict(nb=-1), dict(bl=0), dict(bl=17), dict(cond0=-1),
                 dict(cond0=2), dict(cond0=2 ** 31 - 1), dict(window=-1), dict(sinks=-1), dict(out=None), dict(out=P + 4),
-                dict(hint=-1), dict(ws=None), dict(ws=P + 8), dict(nc=2 ** 30, hint=0), dict(nb=2 ** 30, nc=2 ** 30)):
+                dict(hint=-1), dict(ws=None), dict(ws=P + 8), dict(nc=2 ** 30, hint=0), dict(nb=2 ** 30, nc=2 ** 30),
+                dict(nc=(1 << 18) - 15, hint=0), dict(nc=(1 << 23) // 4, hint=0, batch=8)):
         assert rc(**bad) == 1, bad
     assert rc(window=0, sinks=0 if not four else 3) == 1        # no window: exact pages have a call for that; sinks say nothing then
     assert rc(hint=61) == 3                                     # 61 + 4 > 64

@@ -364,6 +364,87 @@ def test_attention_of_longer_texts(T, four, heads, Ls, rows, window, sinks):
     _run(T, four, heads, BF, Ls, *rows, window, sinks, seed=3).close()
 
 
+def _room(c, pps):
+    """A longer page table, and with it a bound on the prefixes under which the call is planned as a large one."""
+    c.table = torch.cat((c.table, torch.full((c.B, pps - c.pps), -12345, dtype=torch.int32)), 1)
+    c.pps, c.hint = pps, pps * 16 - c.rows[0]
+    return c
+
+
+@pytest.mark.parametrize("four", [True, False])
+@pytest.mark.parametrize("rows", [STEP(5), STEP(7), STEP(16), (37, 1, 8, 37), (40, 2, 5, 0), (128, 0, 1, 0), (150, 1, 3, 150), (1, 1, 16, 1)])
+def test_small_calls_planned_as_large_ones(T, four, rows):
+    """128 rows to a workgroup and pieces of the walks, most of them empty: planned for 65536 positions, filled to a few hundred."""
+    heads = (32, 4, 128) if rows[0] < 30 else (12, 4, 128)
+    for Ls in ([0], [1, 16, 250], [300, 0, 17, 511, 40]):
+        for window, sinks in ((10 ** 6, 0), (10 ** 6, 3)) if not four else ((0, 0),):
+            print(f"large four={four} rows={rows} L={Ls}", flush=True)
+            c = _room(Case(T, four, heads, BF, Ls, *rows, window, sinks, seed=len(Ls)), 4096).build()
+            c.call()
+            c.check()
+            again = c.call(torch.full_like(c.out, 5.0))
+            assert torch.equal(again, c.out)
+            c.close()
+
+
+@pytest.mark.parametrize("four", [True, False])
+@pytest.mark.parametrize("heads,Ls,rows,window,sinks", [
+    ((32, 8, 128), [500, 0, 33, 410, 20, 290, 505], STEP(12), 70, 4),       # 700 workgroups of 128 rows: 512 whole, the others cut
+    ((16, 4, 128), [100] * 8, (200, 1, 16, 200), 0, 0), ((8, 8, 128), [300, 290], (520, 0, 1, 0), 250, 2),
+    ((40, 1, 128), [700, 100, 690], STEP(9), 333, 0), ((12, 2, 128), [1500, 20], STEP(15), 900, 7)])
+def test_many_workgroups_and_windows_of_large_calls(T, four, heads, Ls, rows, window, sinks):
+    print(f"many four={four} {heads} {Ls} {rows} {window} {sinks}", flush=True)
+    if not four and window == 0:
+        window = 10 ** 6
+    c = Case(T, four, heads, BF, Ls, *rows, window, sinks, seed=21)
+    if window == 0 or window >= 10 ** 6:
+        _room(c, 4096)
+    c.build().call()
+    c.check()
+    c.hint = 0                                              # too small a bound: other pieces, the same values within rounding
+    c.ws.fill_(255)
+    c.call()
+    c.check()
+    c.close()
+
+
+@pytest.mark.parametrize("heads,dtype", [((6, 2, 24), F32), ((20, 1, 64), F32), ((40, 1, 128), BF), ((8, 8, 2), F32), ((5, 1, 128), F32)])
+def test_one_token_window(T, heads, dtype):
+    """The step that stores its own row, or, with more than 16 query heads to a kv head, does not."""
+    for Ls in ([0], [15], [16, 31, 900], [64, 0]):
+        for window, sinks in ((1, 0), (16, 1), (300, 20)):
+            print(f"one {heads} {dtype} {Ls} {window}", flush=True)
+            c = _run(T, False, heads, dtype, Ls, 1, 0, 1, 1, window, sinks, seed=31)
+            kp, vp = c.kp.cpu(), c.vp.cpu()
+            for b, L in enumerate(Ls):
+                assert torch.equal(kp[c.ids[b, L // 16], :, L % 16, :], c.kn[b, 0])
+                assert torch.equal(vp[c.ids[b, L // 16], :, :, L % 16], c.vn[b, 0])
+            c.close()
+
+
+@pytest.mark.parametrize("four", [True, False])
+def test_infinities_in_large_calls(T, four):
+    """The same as below, 128 rows to a workgroup."""
+    for what in range(5):
+        c = _room(Case(T, four, (32, 4, 128), BF, [50, 33, 200], 6, 6, 6, 1, 0 if four else 10 ** 6, 0, seed=4), 4096)
+        if what == 0:
+            c.vn[0, 3, :, 1] = math.nan
+        elif what == 1:
+            c.kn[0, 4] = math.nan
+        elif what == 2:
+            c.vn[0, 6 + 6 * 2 + 3, 0, 5] = math.inf
+            c.vn[1, 6 + 6 * 2 + 1, 1, 7] = -math.inf
+        elif what == 3:
+            c.vn[2, 1, :, 2] = math.inf
+            c.vn[2, 4, :, 2] = -math.inf
+        else:
+            c.v[0][1, :, 0] = math.inf
+        c.build()
+        c.call()
+        c.check()
+        c.close()
+
+
 @pytest.mark.parametrize("four", [True, False])
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_scores_that_outgrow_the_reference(T, four, dtype):
