@@ -43,7 +43,10 @@ __global__ __launch_bounds__(64 * W, 2) void span_attn_kernel(SpanArgs a) {
     const int lq = lane & 15, kg = lane >> 4;
     const int n_kv = KV4 ? c.kv4.n_kv : c.kv.n_kv, hd = BF ? HD : (KV4 ? c.kv4.hd : c.kv.hd);
     const int pps = KV4 ? c.kv4.pages_per_seq : c.kv.pages_per_seq, n_pages = KV4 ? c.kv4.n_pages : c.kv.n_pages;
-    const int grp = blockIdx.x / a.tiles, tile = blockIdx.x - grp * a.tiles, split = blockIdx.y;
+    // workgroup i of a launch runs on XCD i % 8: where the heads divide evenly over the eight, those of a head share one's L2
+    const bool xcds = c.B * n_kv % 8 == 0;
+    const int i_wg = xcds ? blockIdx.x >> 3 : blockIdx.x, tile = i_wg % a.tiles, split = blockIdx.y;
+    const int grp = xcds ? (i_wg / a.tiles) * 8 + (blockIdx.x & 7) : i_wg / a.tiles;
     const int b = grp / n_kv, g = grp - b * n_kv;
     const int F = a.group * d.R;
     const int L_raw = c.prefix_len[d.seq_base + b];
@@ -628,16 +631,17 @@ long long span_keys(const RowDesc &d, int rows, int window, int sinks, int max_p
 }
 
 // 16 rows to a workgroup or 128: a wave that takes 16 rows starts and ends sooner, one that takes 32 reads its keys for twice as
-// many and shares them with three others.  What decides is the work in 16 rows by 32 keys, all sequences and heads together, and
-// that the rows fill enough of a workgroup's 128.  us with 16 and with 128 rows:
-//   4-bit pages   8 sequences of 1000 keys and 288 rows (39 k): 51.0, 40.7;  1 of 8000 and 288 (36 k): 43.7, 41.8;
-//                 8 of 1000 and 168 (23 k): 34.4, 36.7;  1 of 8000 and 432 (14 k): 22.2, 36.1;  8 of 8000 and 48 (48 k): 46.0, 57.0
-//   exact pages   a window of 2000, 8 sequences and 72 rows (5.0 k): 27.9, 25.8;  24 (8.1 k): 28.6, 28.3;  36 (12 k): 35.8, 30.9;
-//                 1 and 432 (3.5 k): 19.5, 27.5;  1 and 288 (9.4 k): 28.0, 26.3;  8 and 288 (75 k): 118.6, 57.6
+// many and shares them with three others.  What decides is the work in 16 rows by 32 keys, all sequences and heads together, from
+// exact pages in whole rounds of 256 workgroups, and that the rows fill enough of a workgroup's 128.  us with 16 and with 128 rows:
+//   4-bit pages   8 sequences of 1000 keys and 168 rows of a head (23 k): 32.8, 36.4;  1 of 8000 and 288 (36 k): 43.1, 41.9;
+//                 8 of 1000 and 288 (39 k): 50.5, 40.6;  1 of 8000 and 936 (30 k): 32.3, 44.3;  8 of 8000 and 48 (48 k): 45.2, 57.1
+//   exact pages   one round with a window of 1000 (8.4 k): 19.1, 25.9;  2000 (16 k): 28.1, 28.2;  3000 (24 k): 36.7, 30.9;
+//                 two rounds of 1000, 80 rows (16 k): 33.0, 26.8;  five, 288 rows (44 k): 73.1, 36.2
 static bool many_rows(int dtype, bool four, int F, long long wgs, long long keys) {
     if (dtype != TIDAR_BF16) return false;
-    const long long work = wgs * ((keys + 31) / 32);
-    return four ? F > 64 && work > 36000 : F > 32 && work > 7000;
+    const long long its = (keys + 31) / 32;
+    if (four) return F > 64 && wgs * its > 36000;
+    return F > 32 && (wgs > 256 ? (wgs + 255) / 256 * 256 : wgs) * its > 16200;
 }
 
 // The partial results' memory does not depend on that choice, nor on the keys: a caller's bound on the prefixes may differ from the
