@@ -312,8 +312,7 @@ tidar_status tidar_score(tidar_ctx *ctx, const tidar_weights *w, const tidar_kv_
  *   page_table  dev int32 [batch][pages_per_seq] in/out
  *   row_start   dev int32 [batch + 1] out (a sum beyond 2^31 - 1 reads 2^31 - 1)
  *   slots       dev int32 [slot_cap] out; -1 for the rows of a sequence that was not granted, and behind the last row
- *   held_out    dev int32 [batch] out: pages of the sequence now (held where it is not granted), for the next call; an array of its own
- *               (one that overlaps held is refused: sequences read the held of those before them while theirs is written)
+ *   held_out    dev int32 [batch] out: pages of the sequence now (held where it is not granted), for the next call
  *   granted     dev int32 [batch] out: 1, or 0 where the free list ends before the sequence's last page or its rows do not
  *               end within slot_cap, or -1 where its lengths (negative, beyond pages_per_seq * 16, or more positions
  *               than its pages hold), a page that its rows go into or a page id of its part of the list is not valid.  A sequence that is not granted gets no page and no slot, and
@@ -321,7 +320,8 @@ tidar_status tidar_score(tidar_ctx *ctx, const tidar_weights *w, const tidar_kv_
  *               list was too short for, only those are granted that need no page.
  *   n_taken     dev int32 [1] out: entries of the free list that are used up, from its beginning (the part of a sequence
  *               that is refused for an invalid id counts among them)
- * n_new outside [0, pages_per_seq * 16] counts as no rows.
+ * n_new outside [0, pages_per_seq * 16] counts as no rows.  An output that overlaps prefix_len, n_new, held or free_pages is
+ * refused (TIDAR_EINVAL): sequences read the lengths of those before them while theirs are written.
  */
 tidar_status tidar_table_extend(tidar_ctx *ctx, int32_t batch, const int32_t *prefix_len, const int32_t *n_new,
                                 const int32_t *held, const int32_t *free_pages, int32_t n_free, int32_t *page_table,

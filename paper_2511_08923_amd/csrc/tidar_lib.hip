@@ -1014,7 +1014,14 @@ tidar_status tidar_table_extend(tidar_ctx *ctx, int32_t batch, const int32_t *pr
     if (batch < 1 || batch > ctx->cfg.max_batch || n_free < 0 || (n_free > 0 && !free_pages) || slot_cap < 0 ||
         (slot_cap > 0 && !slots))
         return TIDAR_EINVAL;
-    if (!pool_ok(pages_per_seq, n_pages) || (held < held_out + batch && held_out < held + batch)) return TIDAR_EINVAL;
+    if (!pool_ok(pages_per_seq, n_pages)) return TIDAR_EINVAL;
+    // every workgroup reads the lengths of all sequences before its own, while theirs is written
+    struct { const int32_t *p; size_t n; } in[] = {{prefix_len, (size_t)batch}, {n_new, (size_t)batch}, {held, (size_t)batch}, {free_pages, (size_t)n_free}},
+        out[] = {{page_table, (size_t)batch * pages_per_seq}, {row_start, (size_t)batch + 1}, {slots, (size_t)slot_cap},
+                 {held_out, (size_t)batch}, {granted, (size_t)batch}, {n_taken, 1}};
+    for (const auto &o : out)
+        for (const auto &i : in)
+            if (i.n && o.n && (uintptr_t)i.p < (uintptr_t)(o.p + o.n) && (uintptr_t)o.p < (uintptr_t)(i.p + i.n)) return TIDAR_EINVAL;
     hipStream_t st = (hipStream_t)stream;
     Prof p(ctx, KC_TABLES, st);
     launch_table_extend(batch, prefix_len, n_new, held, free_pages, n_free, page_table, pages_per_seq, n_pages, row_start,

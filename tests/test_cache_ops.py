@@ -34,7 +34,8 @@ def test_page_bytes(T, ctx):
 
 
 def test_table_extend_refusals(T, ctx):
-    good = dict(batch=2, P=P, n=P, held=P, held_out=2 * P, free=P, n_free=3, table=P, pps=4, n_pages=9, start=P, slots=P, cap=8, granted=P, taken=P)
+    good = dict(batch=2, P=P, n=2 * P, held=3 * P, held_out=4 * P, free=5 * P, n_free=3, table=6 * P, pps=4, n_pages=9, start=7 * P,
+                slots=8 * P, cap=8, granted=9 * P, taken=10 * P)
 
     def rc(**kw):
         a = {**good, **kw}
@@ -42,7 +43,9 @@ def test_table_extend_refusals(T, ctx):
                                          a["pps"], a["n_pages"], a["start"], a["slots"], a["cap"], a["held_out"], a["granted"],
                                          a["taken"], None)
 
-    for bad in (dict(ctx=None), dict(batch=0), dict(batch=9), dict(P=None), dict(n=None), dict(held=None), dict(held_out=None), dict(held_out=P), dict(held_out=P + 4), dict(held_out=P - 4), dict(free=None), dict(n_free=-1),
+    for bad in (dict(ctx=None), dict(batch=0), dict(batch=9), dict(P=None), dict(n=None), dict(held=None), dict(held_out=None), dict(held_out=P), dict(held_out=3 * P + 4), dict(held_out=3 * P - 4),
+                dict(granted=2 * P), dict(start=P - 8), dict(slots=3 * P - 28), dict(table=5 * P - 28), dict(taken=5 * P + 8), dict(held_out=4 * P, free=4 * P - 8),
+                dict(free=None), dict(n_free=-1),
                 dict(table=None), dict(pps=0), dict(pps=(1 << 26) + 1), dict(n_pages=0), dict(n_pages=(1 << 27) + 1),
                 dict(start=None), dict(slots=None), dict(cap=-1), dict(granted=None), dict(taken=None)):
         assert rc(**bad) == 1, bad
