@@ -154,9 +154,10 @@ __global__ __launch_bounds__(256) void table_extend_kernel(TableArgs a) {
 }
 
 // ------------------------------------------------------------------ rows into 4-bit pages and back
-// A lane takes eight elements (16 bytes of bf16), the four lanes of a block agree on its scale by two shuffles, and a wave
-// takes four rows of a head at head_dim 128: its stores into V's token quads are then whole runs of 16 bytes where the rows
-// are neighbours.  Bound by the bytes of the rows.
+// A lane takes eight elements (16 bytes of bf16), the four lanes of a block agree on its scale by two shuffles, and 16 rows of a
+// head follow one another: of rows that are neighbours a workgroup holds whole pages, whose lines then go through one XCD's L2
+// (four rows at a time 16000 rows of 8 heads took 29.0 us to store and 21.9 to load, sixteen 25.8 and 14.0; pages put together in LDS
+// and written 16 bytes a lane 27.1).  Bound by the bytes of the rows.
 struct RowArgs {
     Kv4View kv;
     const int32_t *slots;
@@ -167,12 +168,12 @@ __device__ inline bool row_piece(const RowArgs &a, size_t idx, int &row, int &h,
     const int ng = 4 * kv4_blocks(a.kv.hd);
     grp = (int)(idx % ng);
     const size_t t = idx / ng;
-    const int rr = (int)(t & 3);
-    const size_t u = t >> 2;
+    const int rr = (int)(t & 15);
+    const size_t u = t >> 4;
     h = (int)(u % a.kv.n_kv);
     const size_t rb = u / a.kv.n_kv;
-    row = (int)(rb * 4 + rr);
-    return rb * 4 + rr < (size_t)a.n_rows;
+    row = (int)(rb * 16 + rr);
+    return rb * 16 + rr < (size_t)a.n_rows;
 }
 
 template <typename T>
@@ -239,7 +240,7 @@ __global__ __launch_bounds__(256) void kv4_store_kernel(RowArgs a, const T *__re
     }
 }
 
-// ONCE: more than the L2s hold together, written past them (16000 rows of 8 heads: 16.1 -> 13.4 us)
+// ONCE: more than the L2s hold together, written past them (16000 rows of 8 heads, store and load: 46.7 us a pass, without it 54)
 template <typename T, bool ONCE>
 __global__ __launch_bounds__(256) void kv4_load_kernel(RowArgs a, T *__restrict__ k, T *__restrict__ v) {
     const int nb = kv4_blocks(a.kv.hd), hd = a.kv.hd;
@@ -391,7 +392,7 @@ static RowArgs row_args(const Kv4View &kv, const int32_t *slots, int n_rows, con
     return {kv, slots, n_rows, kv.hd % 8 == 0 && (((uintptr_t)k | (uintptr_t)v) & 15) == 0};
 }
 static dim3 row_grid(const Kv4View &kv, int n_rows) {
-    const size_t lanes = (size_t)((n_rows + 3) / 4) * 4 * kv.n_kv * 4 * kv4_blocks(kv.hd);
+    const size_t lanes = ((size_t)n_rows + 15) / 16 * 16 * kv.n_kv * 4 * kv4_blocks(kv.hd);
     return dim3((unsigned)((lanes + 255) / 256));
 }
 void launch_kv4_store(int dtype, const Kv4View &kv, const int32_t *slots, int n_rows, const void *k, const void *v,
