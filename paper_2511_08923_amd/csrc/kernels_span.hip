@@ -151,6 +151,7 @@ __global__ __launch_bounds__(64 * W, 2) void span_attn_kernel(SpanArgs a) {
         if ((unsigned)page >= (unsigned)n_pages) return;
         const size_t at = ((size_t)page * n_kv + g) * 16 * hd;
         T *kd = (T *)const_cast<void *>(c.kv.k_pages) + at + (L & 15) * hd, *vd = (T *)const_cast<void *>(c.kv.v_pages) + at + (L & 15);
+#pragma unroll 1
         for (int e = lane; e < hd; e += 64) {
             kd[e] = ((const T *)c.k_one)[new_row + e];
             vd[(size_t)e * 16] = ((const T *)c.v_one)[new_row + e];
@@ -305,18 +306,19 @@ __global__ __launch_bounds__(64 * W, 2) void span_attn_kernel(SpanArgs a) {
                     const int key = (u1 == new_unit ? 16 : 0) + (L & 15);        // of the 32: tile t, row 4a + e is key 8a + 4t + e
                     const bf16_t *kn = (const bf16_t *)c.k_one + new_row, *vn = (const bf16_t *)c.v_one + new_row;
 #pragma unroll
-                    for (int t = 0; t < 2; ++t)
-                        if (8 * (lq >> 2) + 4 * t + (lq & 3) == key)
+                    for (int j = 0; j < 4; ++j) {
+                        bf16x8 y;                        // (the row need not be aligned)
 #pragma unroll
-                            for (int j = 0; j < 4; ++j)
+                        for (int e = 0; e < 8; ++e) y[e] = kn[32 * j + 8 * kg + e];
 #pragma unroll
-                                for (int e = 0; e < 8; ++e) x.k[t][j][e] = kn[32 * j + 8 * kg + e];
-                    if ((key >> 3) == kg)
+                        for (int t = 0; t < 2; ++t) x.k[t][j] = 8 * (lq >> 2) + 4 * t + (lq & 3) == key ? y : x.k[t][j];
+                    }
 #pragma unroll
-                        for (int t = 0; t < HT; ++t)
+                    for (int t = 0; t < HT; ++t) {
+                        const bf16_t y = vn[16 * t + lq];
 #pragma unroll
-                            for (int e = 0; e < 8; ++e)
-                                if (e == (key & 7)) x.v[t][e] = vn[16 * t + lq];
+                        for (int e = 0; e < 8; ++e) x.v[t][e] = 8 * kg + e == key ? y : x.v[t][e];
+                    }
                     store_new();
                 }
                 body(whole, x.k, x.v, vis);
@@ -344,14 +346,15 @@ __global__ __launch_bounds__(64 * W, 2) void span_attn_kernel(SpanArgs a) {
     } else {
         // ---- fp32: 16x16x4 MFMAs.  A lane's head-dim values of O^T tile t are HT i + t.
         const bool vec = hd % 4 == 0;
-        auto load_k = [&](const float *kp, float (&k)[Q4]) __attribute__((always_inline)) {      // token lq of a tile [16][hd]
-            const float *src = kp + lq * hd + Q4 * kg;
+        typedef f32x4 any_f32x4 __attribute__((aligned(4)));     // (a new row need not be aligned)
+        auto load_k = [&](const float *kp, float (&k)[Q4]) __attribute__((always_inline)) {      // token lq: hd values from kp on
+            const float *src = kp + Q4 * kg;
             const int n = hd - Q4 * kg;
 #pragma unroll
             for (int j = 0; j < Q4; j += 4) {
                 f32x4 x = {0.f, 0.f, 0.f, 0.f};
                 if (vec) {
-                    if (j < n) x = *(const f32x4 *)(src + j);
+                    if (j < n) x = *(const any_f32x4 *)(src + j);
                 } else {
 #pragma unroll
                     for (int e = 0; e < 4; ++e) x[e] = j + e < n ? src[j + e] : 0.f;
@@ -415,24 +418,34 @@ __global__ __launch_bounds__(64 * W, 2) void span_attn_kernel(SpanArgs a) {
             for (int t = 0; t < HT; ++t)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) top = max(top, __float_as_uint(v[t][e]) & 0x7fffffffu);
-            if (__builtin_expect(__any(top >= 0x7f800000u), 0)) {
+            if (__builtin_expect(__any(top >= 0x7f800000u), 0)) {        // as above: set aside, and added key by key
+                float (*vl)[HD + 4] = red[wave];
+                unsigned mine = 0, keys = 0;
 #pragma unroll
-                for (int t = 0; t < HT; ++t) {
-                    f32x4 n_pos = {0.f, 0.f, 0.f, 0.f}, n_neg = n_pos, n_nan = n_pos;
+                for (int e = 0; e < 4; ++e)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float x = v[t][e], seen = (float)((vis16 >> (4 * kg + e)) & 1u);
-                        n_pos = __builtin_amdgcn_mfma_f32_16x16x4f32(x == INFINITY ? 1.f : 0.f, seen, n_pos, 0, 0, 0);
-                        n_neg = __builtin_amdgcn_mfma_f32_16x16x4f32(x == -INFINITY ? 1.f : 0.f, seen, n_neg, 0, 0, 0);
-                        n_nan = __builtin_amdgcn_mfma_f32_16x16x4f32(x != x ? 1.f : 0.f, seen, n_nan, 0, 0, 0);
-                        v[t][e] = fabsf(x) < INFINITY ? x : 0.f;
+                    for (int t = 0; t < HT; ++t) {
+                        vl[4 * kg + e][HT * lq + t] = v[t][e];
+                        if (!(fabsf(v[t][e]) < INFINITY)) {
+                            mine |= 1u << e;
+                            v[t][e] = 0.f;
+                        }
                     }
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (n_pos[e] > 0.f) acc[t][e] += INFINITY;
-                        if (n_neg[e] > 0.f) acc[t][e] -= INFINITY;
-                        if (n_nan[e] > 0.f) acc[t][e] = __builtin_nanf("");
-                    }
+                for (int o = 1; o < 16; o <<= 1) mine |= __shfl_xor(mine, o);
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4) keys |= __builtin_amdgcn_readlane(mine, 16 * q4) << (4 * q4);
+#pragma unroll 1
+                for (int key = 0; key < 16; ++key) {
+                    const bool seen = (vis16 >> key) & 1u;
+                    if (!((keys >> key) & 1u) || !__any(seen)) continue;
+#pragma unroll
+                    for (int t = 0; t < HT; ++t)
+#pragma unroll
+                        for (int r4 = 0; r4 < 4; ++r4) {
+                            const float x = vl[key][HT * (4 * kg + r4) + t];
+                            acc[t][r4] += seen && !(fabsf(x) < INFINITY) ? x : 0.f;
+                        }
                 }
             }
 #pragma unroll
@@ -453,11 +466,8 @@ __global__ __launch_bounds__(64 * W, 2) void span_attn_kernel(SpanArgs a) {
                 const size_t piece = cache ? (size_t)page_of(n, t) * n_kv + g : ((size_t)b * n_kv + g) * n_mt + max(u[t], 0);
                 at[t] = piece * 16 * hd;
                 if (KV4 && cache) load_k4(c.kv4.pages + piece * kv4_head_bytes(hd), k);
-                else load_k((const float *)(cache ? c.kv.k_pages : c.k_scr) + at[t], k);
-                if (cache && u[t] == new_unit && lq == (L & 15)) {
-#pragma unroll
-                    for (int j = 0; j < Q4; ++j) k[j] = Q4 * kg + j < hd ? ((const float *)c.k_one)[new_row + Q4 * kg + j] : 0.f;
-                }
+                else load_k(!KV4 && cache && u[t] == new_unit && lq == (L & 15) ? (const float *)c.k_one + new_row
+                                : (const float *)(cache ? c.kv.k_pages : c.k_scr) + at[t] + lq * hd, k);
                 if (KV4 && cache) at[t] = piece * kv4_head_bytes(hd);
                 s[t] = scores(k);
             }
@@ -469,13 +479,13 @@ __global__ __launch_bounds__(64 * W, 2) void span_attn_kernel(SpanArgs a) {
             for (int t = 0; t < 2; ++t) {
                 if (KV4 && cache) load_v4(c.kv4.pages + at[t], v);
                 else load_v((const float *)(cache ? c.kv.v_pages : c.v_scr) + at[t], v);
-                if (cache && u[t] == new_unit) {
-                    if (((L & 15) >> 2) == kg)
+                if (!KV4 && cache && u[t] == new_unit) {
 #pragma unroll
-                        for (int i = 0; i < HT; ++i)
+                    for (int i = 0; i < HT; ++i) {
+                        const float y = HT * lq + i < hd ? ((const float *)c.v_one)[new_row + HT * lq + i] : 0.f;
 #pragma unroll
-                            for (int e = 0; e < 4; ++e)
-                                if (e == (L & 3) && HT * lq + i < hd) v[i][e] = ((const float *)c.v_one)[new_row + HT * lq + i];
+                        for (int e = 0; e < 4; ++e) v[i][e] = 4 * kg + e == (L & 15) ? y : v[i][e];
+                    }
                     store_new();
                 }
                 weigh(v, p + 4 * t, vis >> (16 * t));

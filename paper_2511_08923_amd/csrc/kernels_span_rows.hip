@@ -388,9 +388,10 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
         }
     };
 
-    // Tiles to come.  At the start of iteration n the codes of tile n + 5 (4-bit pages) or tile n + 3 itself (exact pages) are
-    // asked for; at its end tile n + 3 is converted, or tile n + 1 has landed.
-    Raw r0 = {}, r1 = {}, r2 = {};
+    // Tiles to come.  Exact pages: at the start of iteration n tile n + 3 is asked for, at its end tile n + 1 has landed.  4-bit
+    // pages: at the end of iteration n the codes of tile n + 3 are converted and those of tile n + 5 asked for in their place: the
+    // iterations take turns with two sets of registers (handed on from one to the next, a copy would wait for the newest load)
+    Raw r0 = {}, r1 = {};
     if constexpr (KV4) {
 #pragma unroll
         for (int m = 0; m < 3; ++m) stage4(m, fetch(page_at(m)));
@@ -405,33 +406,42 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
     wait_loads<0>();
     lds_barrier();
     auto begin = [&](int n) __attribute__((always_inline)) {
-        if constexpr (KV4) r2 = fetch(page_at(n + 5));
-        else ask(n + 3, page_at(n + 3));
+        if constexpr (!KV4) ask(n + 3, page_at(n + 3));
     };
-    auto finish = [&](int n) __attribute__((always_inline)) {
+    auto finish = [&](int n, Raw &x) __attribute__((always_inline)) {
         if constexpr (KV4) {
-            stage4(n + 3, r0);
-            r0 = r1;
-            r1 = r2;
+            stage4(n + 3, x);
+            x = fetch(page_at(n + 5));
         } else {
             wait_loads<8>();
         }
         lds_barrier_counted();
     };
-    if (!here) {                                         // no rows: this wave only moves tiles
+    auto take_turns = [&](auto &turn) __attribute__((always_inline)) {
         for (int n = 0; n < n_seq; ++n) {
-            begin(n);
-            finish(n);
+            turn(n, r0);
+            if constexpr (KV4) {
+                if (++n == n_seq) break;
+                turn(n, r1);
+            }
         }
+    };
+    if (!here) {                                         // no rows: this wave only moves tiles
+        auto turn = [&](int n, Raw &x) __attribute__((always_inline)) {
+            begin(n);
+            finish(n, x);
+        };
+        take_turns(turn);
     } else {
         // blocks [f0, f1) are cache units that every row of the wave sees whole: no predicate there
         const int base = wk.w0 - wk.n_s + 2 * it0;
         const int f0 = max(((wk.n_s + 1) >> 1) - it0, ((((rb.lo1 + 15) >> 4) - base) + 1) >> 1), f1 = ((rb.hi0 >> 4) - base) >> 1;
-        for (int n = 0; n < n_seq; ++n) {
+        auto turn = [&](int n, Raw &x) __attribute__((always_inline)) {
             begin(n);
             f32x16 s;
             scores(n, s);
-            bf16x8 vf[4][2], pf[2];
+            bf16x8 vf[4][2];
+            u32x4 pw[2];
             v_frags(n, vf);
             unsigned vis = 0;
             const bool masked = n < f0 || n >= f1;
@@ -468,15 +478,16 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
                 const bf16x2 pk = {(bf16_t)__builtin_amdgcn_exp2f(fmaf(s[e], scale, -m_safe)),
                                    (bf16_t)__builtin_amdgcn_exp2f(fmaf(s[e + 1], scale, -m_safe))};
                 l_run = __builtin_amdgcn_fdot2_f32_bf16(pk, ones, l_run, false);
-                pf[e >> 3][e & 7] = pk[0];
-                pf[e >> 3][(e & 7) + 1] = pk[1];
+                pw[e >> 3][(e & 7) >> 1] = __builtin_bit_cast(unsigned, pk);
             }
+            const bf16x8 pf[2] = {__builtin_bit_cast(bf16x8, pw[0]), __builtin_bit_cast(bf16x8, pw[1])};
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int t = 0; t < 4; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[t][u], pf[u], acc[t], 0, 0, 0);
-            finish(n);
-        }
+            finish(n, x);
+        };
+        take_turns(turn);
     }
 
     // ---- results
