@@ -670,12 +670,14 @@ SpanPlan plan_span(int dtype, bool four, int B, int n_q, int n_kv, int hd, const
     p.tiles = (F + 15) / 16;
     // One round of workgroups, eight waves to a compute unit.  A wave's iteration takes about 0.75 us, the join of the splits 3 and
     // 4 ns per partial result: the least sum wins.  (us at 1, 2, 4, 8, 16 splits: 32 sequences of 1000 keys in 4 bits 12.1, 19.5,
-    // 25.8, 37.5, 65.6; 8 of 8192 40.3, 26.5, 19.8, 25.3, 33.9; one over an exact window of 4096 43.5, 30.0, 19.8, 13.3, 11.3)
+    // 25.8, 37.5, 65.6; 8 of 8192 40.3, 26.5, 19.8, 25.3, 33.9; one over an exact window of 4096 43.5, 30.0, 19.8, 13.3, 11.3.)  fp32
+    // waits for each tile: 3 us (72 rows over 570 keys of head_dim 128: 43 us unsplit, 22 in five)
     const int per_it = 32 * span_waves(dtype), bound = most_splits(dtype, wgs);
     p.splits = 1;
+    const double it_us = dtype == TIDAR_BF16 ? 0.75 : 3.0;
     double best = 0.0;
     for (int s = 1; s <= bound; ++s) {
-        const double t = 0.75 * (double)((keys + per_it * s - 1) / (per_it * s)) + (s > 1 ? 3.0 + 0.004 * (double)wgs * s : 0.0);
+        const double t = it_us * (double)((keys + per_it * s - 1) / (per_it * s)) + (s > 1 ? 3.0 + 0.004 * (double)wgs * s : 0.0);
         if (s == 1 || t < best) {
             best = t;
             p.splits = s;
