@@ -304,9 +304,10 @@ tidar_status tidar_score(tidar_ctx *ctx, const tidar_weights *w, const tidar_kv_
 /*
  * Page table entries and slots for the rows that every sequence is about to get (a prompt's chunk, a draft, one token).
  * Sequence b holds positions [0, prefix_len[b]), its row of the table has held[b] pages (also such as rejected drafts left
- * behind), and it gets n_new[b] rows at prefix_len[b].  The pages that are missing, entries held .. ceil((prefix_len + n_new)/16) - 1,
- * are taken from the free list in the order of the sequences; no other entry is written.  The new rows of all sequences are numbered one after another:
- * sequence b has rows row_start[b] .. row_start[b + 1] - 1, and slots[] holds where each goes.
+ * behind), and it gets n_new[b] rows at prefix_len[b].  The pages that are missing, entries
+ * held .. ceil((prefix_len + n_new)/16) - 1, are taken from the free list in the order of the sequences; no other entry is
+ * written.  The new rows of all sequences are numbered one after another: sequence b has rows row_start[b] ..
+ * row_start[b + 1] - 1, and slots[] holds where each goes.
  *   prefix_len, n_new, held   dev int32 [batch]; prefix_len is not changed (the attention calls take the same)
  *   free_pages  dev int32 [n_free]: ids of free pages, each once (NULL with n_free 0); the list is not changed
  *   page_table  dev int32 [batch][pages_per_seq] in/out
@@ -315,9 +316,10 @@ tidar_status tidar_score(tidar_ctx *ctx, const tidar_weights *w, const tidar_kv_
  *   held_out    dev int32 [batch] out: pages of the sequence now (held where it is not granted), for the next call
  *   granted     dev int32 [batch] out: 1, or 0 where the free list ends before the sequence's last page or its rows do not
  *               end within slot_cap, or -1 where its lengths (negative, beyond pages_per_seq * 16, or more positions
- *               than its pages hold), a page that its rows go into or a page id of its part of the list is not valid.  A sequence that is not granted gets no page and no slot, and
- *               nothing of its row of the table is written; it may be tried again.  Sequences do not overtake: behind one that the
- *               list was too short for, only those are granted that need no page.
+ *               than its pages hold), a page that its rows go into or a page id of its part of the list is not valid.  A
+ *               sequence that is not granted gets no page and no slot, and nothing of its row of the table is written; it may
+ *               be tried again.  Sequences do not overtake: behind one that the list was too short for, only those are granted
+ *               that need no page.
  *   n_taken     dev int32 [1] out: entries of the free list that are used up, from its beginning (the part of a sequence
  *               that is refused for an invalid id counts among them)
  * n_new outside [0, pages_per_seq * 16] counts as no rows.  An output that overlaps prefix_len, n_new, held or free_pages is

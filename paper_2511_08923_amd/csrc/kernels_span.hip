@@ -9,15 +9,16 @@
 // units of 16 keys (cache pages, then mask tiles) that any of its rows sees; any two units make an iteration of 32 keys.  Pages
 // between the sinks and the window are never read, not even their table entries.  The waves take
 // turns with the iterations, each with its own softmax state, straight from memory into registers (no LDS, no barrier in the loop),
-// and are folded through LDS at the end.  Where the tiles do not fill the chip the walk is cut into key splits, evenly by its real length, and the partial
-// results are joined by a second kernel.
+// and are folded through LDS at the end.  Where the tiles do not fill the chip the walk is cut into key splits, evenly by its
+// real length, and the partial results are joined by a second kernel.  Bound by the bytes where few rows read many keys (32
+// sequences of up to 8192 4-bit keys, one token each: 49 us, 4.4 TB/s), else by what a wave waits for (8 waves to a unit).
 //
 // The softmax.  Scores are formed transposed, S^T[key][q], so that a lane holds one query row's scores of its keys and they are,
 // without moving, the B operand of O^T[d][q] += V^T[d][key] P^T[key][q].  Numerators are taken against a power of two that is
 // moved only when the scores outgrow it by 2^16 (and from -inf by a row's first key): every rescale is exact, and no common
 // path reduces a maximum across lanes.  (A reference may lag behind the waves' and splits' common maximum by the 2^16, and
-// what is folded with a factor below 2^-126 is lost: weights below 2^-110 of a row's largest.)  bf16: numerators are rounded to bf16 for the matrix product (relative 2^-9, as in
-// tidar_hybrid_attention) and the denominator sums the rounded values in fp32.
+// what is folded with a factor below 2^-126 is lost: weights below 2^-110 of a row's largest.)  bf16: numerators are rounded to
+// bf16 for the matrix product (relative 2^-9, as in tidar_hybrid_attention) and the denominator sums the rounded values in fp32.
 //
 // What a masked place holds never shows: scores are replaced by -inf, and infinities and NaN of V, which a weight of zero would
 // turn into NaN, are taken out of the product in units that are not wholly visible, and put back for the rows that see them.
@@ -471,7 +472,8 @@ __global__ __launch_bounds__(64 * W, 2) void span_attn_kernel(SpanArgs a) {
                 if (KV4 && cache) at[t] = piece * kv4_head_bytes(hd);
                 s[t] = scores(k);
             }
-            const unsigned vis = cache ? cache_bits(rs, u[0]) | (cache_bits(rs, u[1]) << 16) : mask_bits(rs, u[0]) | (mask_bits(rs, u[1]) << 16);
+            const unsigned vis = cache ? cache_bits(rs, u[0]) | (cache_bits(rs, u[1]) << 16)
+                                       : mask_bits(rs, u[0]) | (mask_bits(rs, u[1]) << 16);
             softmax(false, s, vis, p);
 #pragma unroll
             for (int e = 0; e < 8; ++e) l_run += p[e];
