@@ -205,12 +205,14 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
         if (row) qf[ks] = *(const bf16x8 *)((const bf16_t *)c.q + orh * HD + 8 * lh + 16 * ks);
     }
     const float scale = kLog2e / sqrtf((float)HD);
+    const float inv_scale = 1.f / scale;
     f32x16 acc[4];
 #pragma unroll
     for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[t][e] = 0.f;
     float m_run = -INFINITY, l_run = 0.f;
+    float m_neg = 0.f, m_most = -INFINITY;               // what is added to scores; scores beyond which the reference moves
 
     // ---- staging: wave w moves unit w / 2 of a tile's pair, of it K rows 8 (w % 2) .. + 7 and V key half w % 2
     const int u_w = wave >> 1, half_w = wave & 1;
@@ -302,17 +304,17 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
     };
     // 4-bit pages: tile m into its slot of the ring, from registers, or, mask rows, by direct loads (rare: waited for at once).  A tile
     // that there is not is written all the same: its slot is free
-    auto stage4 = [&](int m, const Raw &x) __attribute__((always_inline)) {
-        convert(x, m & (RING - 1));
+    auto stage4 = [&](int m, int slot, const Raw &x) __attribute__((always_inline)) {
+        convert(x, slot);
         if (m < n_seq && it0 + m >= wk.n1) {
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");           // what this wave just wrote must not come later
-            dma_k(dks, mask_base(m), m & (RING - 1));
-            dma_v(dvs, mask_base(m), m & (RING - 1));
+            dma_k(dks, mask_base(m), slot);
+            dma_v(dvs, mask_base(m), slot);
             wait_loads<0>();
         }
     };
     // exact pages and mask rows: four direct loads of tile m; of a tile that there is not, through a buffer of no bytes
-    auto ask = [&](int m, int page) __attribute__((always_inline)) {
+    auto ask = [&](int m, int slot, int page) __attribute__((always_inline)) {
         const bool mask = it0 + m >= wk.n1;
         int4v kd, vd;
 #pragma unroll
@@ -323,13 +325,13 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
         kd[2] = m < n_seq ? kd[2] : 0;
         vd[2] = m < n_seq ? vd[2] : 0;
         const int base = mask ? mask_base(m) : page_base(page);
-        dma_k(kd, base, m & (RING - 1));
-        dma_v(vd, base, m & (RING - 1));
+        dma_k(kd, base, slot);
+        dma_v(vd, base, slot);
     };
 
     // K as A operand: lane = (tile row, half of the step); V^T as A operand: lane = (position, key half of the unit)
-    auto k_frags = [&](int m, bf16x8 (&kf)[8]) __attribute__((always_inline)) {
-        const unsigned char *p = reinterpret_cast<const unsigned char *>(&k_lds[m & (RING - 1)][0]) + lq * 256;
+    auto k_frags = [&](int slot, bf16x8 (&kf)[8]) __attribute__((always_inline)) {
+        const unsigned char *p = reinterpret_cast<const unsigned char *>(&k_lds[slot][0]) + lq * 256;
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) kf[ks] = *(const bf16x8 *)(p + (((2 * ks + lh) ^ (lq & 15)) << 4));
     };
@@ -339,8 +341,8 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks) s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[ks], qf[ks], s, 0, 0, 0);
     };
-    auto v_frags = [&](int m, bf16x8 (&vf)[4][2]) __attribute__((always_inline)) {
-        const unsigned char *p = reinterpret_cast<const unsigned char *>(&v_lds[m & (RING - 1)][0]);
+    auto v_frags = [&](int slot, bf16x8 (&vf)[4][2]) __attribute__((always_inline)) {
+        const unsigned char *p = reinterpret_cast<const unsigned char *>(&v_lds[slot][0]);
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
@@ -349,7 +351,7 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
     // V^T values that are not finite, of a block that not every row sees whole: taken out of the fragments, and added for the
     // rows that see them, key by key from LDS (rare, and written to need few registers; what lies in slots that no row
     // sees, unset memory perhaps, costs the first step only)
-    auto set_aside = [&](int m, bf16x8 (&vf)[4][2], unsigned vis) __attribute__((always_inline)) {
+    auto set_aside = [&](int slot, bf16x8 (&vf)[4][2], unsigned vis) __attribute__((always_inline)) {
         unsigned odd = 0;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
@@ -359,7 +361,7 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
                 odd |= nonfinite2(w[0]) | nonfinite2(w[1]) | nonfinite2(w[2]) | nonfinite2(w[3]);
             }
         if (__builtin_expect(__any(odd != 0), 0)) {
-            const unsigned short *v = reinterpret_cast<const unsigned short *>(&v_lds[m & (RING - 1)][0]);
+            const unsigned short *v = reinterpret_cast<const unsigned short *>(&v_lds[slot][0]);
             unsigned keys = 0;                           // this lane's: bit 8 u + e
 #pragma unroll
             for (int t = 0; t < 4; ++t)
@@ -395,67 +397,71 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
     Raw r0 = {}, r1 = {};
     if constexpr (KV4) {
 #pragma unroll
-        for (int m = 0; m < 3; ++m) stage4(m, fetch(page_at(m)));
+        for (int m = 0; m < 3; ++m) stage4(m, m, fetch(page_at(m)));
         r0 = fetch(page_at(3));
         r1 = fetch(page_at(4));
     } else {
 #pragma unroll
-        for (int m = 0; m < 3; ++m) ask(m, page_at(m));
+        for (int m = 0; m < 3; ++m) ask(m, m, page_at(m));
     }
 #pragma unroll
     for (int ks = 0; ks < 8; ++ks) asm volatile("" : "+v"(qf[ks]));      // no wait for Q inside the loop
     wait_loads<0>();
     lds_barrier();
-    auto begin = [&](int n) __attribute__((always_inline)) {
-        if constexpr (!KV4) ask(n + 3, page_at(n + 3));
+    auto begin = [&](int n, int slot) __attribute__((always_inline)) {
+        if constexpr (!KV4) ask(n + 3, (slot + 3) % RING, page_at(n + 3));
     };
-    auto finish = [&](int n, Raw &x) __attribute__((always_inline)) {
+    auto finish = [&](int n, int slot, Raw &x) __attribute__((always_inline)) {
         if constexpr (KV4) {
-            stage4(n + 3, x);
+            stage4(n + 3, (slot + 3) % RING, x);
             x = fetch(page_at(n + 5));
         } else {
             wait_loads<4>();
         }
         lds_barrier_counted();
     };
+    // four iterations at a time: a tile's place in the ring is then part of the LDS instructions (274.5 -> 267.5 us)
     auto take_turns = [&](auto &turn) __attribute__((always_inline)) {
         for (int n = 0; n < n_seq; ++n) {
-            turn(n, r0);
-            if constexpr (KV4) {
-                if (++n == n_seq) break;
-                turn(n, r1);
-            }
+            turn(n, 0, r0);
+            if (++n == n_seq) break;
+            turn(n, 1, r1);
+            if (++n == n_seq) break;
+            turn(n, 2, r0);
+            if (++n == n_seq) break;
+            turn(n, 3, r1);
         }
     };
     if (!here) {                                         // no rows: this wave only moves tiles
-        auto turn = [&](int n, Raw &x) __attribute__((always_inline)) {
-            begin(n);
-            finish(n, x);
+        auto turn = [&](int n, int slot, Raw &x) __attribute__((always_inline)) {
+            begin(n, slot);
+            finish(n, slot, x);
         };
         take_turns(turn);
     } else {
         // blocks [f0, f1) are cache units that every row of the wave sees whole: no predicate there
         const int base = wk.w0 - wk.n_s + 2 * it0;
-        const int f0 = max(((wk.n_s + 1) >> 1) - it0, ((((rb.lo1 + 15) >> 4) - base) + 1) >> 1), f1 = ((rb.hi0 >> 4) - base) >> 1;
+        const int f0 = __builtin_amdgcn_readfirstlane(max(((wk.n_s + 1) >> 1) - it0, ((((rb.lo1 + 15) >> 4) - base) + 1) >> 1));
+        const int f1 = __builtin_amdgcn_readfirstlane(((rb.hi0 >> 4) - base) >> 1);
         // exact pages: K of tile n + 1 is read while tile n's numerators are formed (69.2 -> 66.7 us for a pass of 2064 rows of 32
         // heads; 4-bit pages have no registers for it: 277.8 -> 291.7 us)
         bf16x8 k_next[8];
         if constexpr (!KV4) k_frags(0, k_next);
-        auto turn = [&](int n, Raw &x) __attribute__((always_inline)) {
-            begin(n);
+        auto turn = [&](int n, int slot, Raw &x) __attribute__((always_inline)) {
+            begin(n, slot);
             f32x16 s;
             bf16x8 vf[4][2];
             u32x4 pw[2];
             if constexpr (KV4) {                         // (all eight reads before the first product: 278.0 -> 275.4 us)
                 bf16x8 kf[8];
-                k_frags(n, kf);
+                k_frags(slot, kf);
                 __builtin_amdgcn_sched_barrier(0);
                 scores(kf, s);
-                v_frags(n, vf);
+                v_frags(slot, vf);
             } else {
                 scores(k_next, s);
-                v_frags(n, vf);
-                k_frags(n + 1, k_next);
+                v_frags(slot, vf);
+                k_frags((slot + 1) % RING, k_next);
             }
             unsigned vis = 0;
             const bool masked = n < f0 || n >= f1;
@@ -474,9 +480,9 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
             float mx = -INFINITY;
 #pragma unroll
             for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[e]);
-            if (__builtin_expect(__any(!(mx * scale <= m_run + kLag)), 0)) {
+            if (__builtin_expect(__any(!(mx <= m_most)), 0)) {
                 mx = fmaxf(mx, __shfl_xor(mx, 32));
-                if (!(mx * scale <= m_run + kLag)) {
+                if (!(mx <= m_most)) {
                     const float m_new = fmaxf(m_run, ceilf(mx * scale)), alpha = __builtin_amdgcn_exp2f(m_run - m_new);
                     l_run *= alpha;
 #pragma unroll
@@ -484,15 +490,16 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
 #pragma unroll
                         for (int e = 0; e < 16; ++e) acc[t][e] *= alpha;
                     m_run = m_new;
+                    m_neg = m_new == -INFINITY ? 0.f : -m_new;
+                    m_most = (m_new + kLag) * inv_scale;
                 }
             }
-            if (masked) set_aside(n, vf, vis);           // (behind the rescale: a factor of zero would make NaN of infinity)
-            const float m_safe = m_run == -INFINITY ? 0.f : m_run;
+            if (masked) set_aside(slot, vf, vis);           // (behind the rescale: a factor of zero would make NaN of infinity)
             const bf16x2 ones = {(bf16_t)1.0f, (bf16_t)1.0f};
 #pragma unroll
             for (int e = 0; e < 16; e += 2) {
-                const bf16x2 pk = {(bf16_t)__builtin_amdgcn_exp2f(fmaf(s[e], scale, -m_safe)),
-                                   (bf16_t)__builtin_amdgcn_exp2f(fmaf(s[e + 1], scale, -m_safe))};
+                const bf16x2 pk = {(bf16_t)__builtin_amdgcn_exp2f(fmaf(s[e], scale, m_neg)),
+                                   (bf16_t)__builtin_amdgcn_exp2f(fmaf(s[e + 1], scale, m_neg))};
                 l_run = __builtin_amdgcn_fdot2_f32_bf16(pk, ones, l_run, false);
                 pw[e >> 3][(e & 7) >> 1] = __builtin_bit_cast(unsigned, pk);
             }
@@ -502,7 +509,7 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
             for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int t = 0; t < 4; ++t) acc[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[t][u], pf[u], acc[t], 0, 0, 0);
-            finish(n, x);
+            finish(n, slot, x);
         };
         take_turns(turn);
     }
