@@ -181,13 +181,13 @@ __global__ __launch_bounds__(64 * W, 2) void span_attn_kernel(SpanArgs a) {
                 pf[e + 1] = pk[1];
             }
             if (!whole) {
-                unsigned odd = 0;
+                unsigned top = 0;
 #pragma unroll
                 for (int t = 0; t < HT; ++t) {
                     const u32x4 w = __builtin_bit_cast(u32x4, vf[t]);
-                    odd |= nonfinite2(w[0]) | nonfinite2(w[1]) | nonfinite2(w[2]) | nonfinite2(w[3]);
+                    top = top2(top2(top2(top2(top, w[0]), w[1]), w[2]), w[3]);
                 }
-                if (__builtin_expect(__any(odd != 0), 0)) {
+                if (__builtin_expect(__any(nonfinite2(top) != 0), 0)) {
                     // taken out of the fragments, and added for the rows that see them, key by key through the wave's share of
                     // LDS (rare, and written to need few registers; what lies in slots that no row sees costs the first step only)
                     unsigned short *v = reinterpret_cast<unsigned short *>(&red[wave][0][0]);

@@ -352,15 +352,15 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
     // rows that see them, key by key from LDS (rare, and written to need few registers; what lies in slots that no row
     // sees, unset memory perhaps, costs the first step only)
     auto set_aside = [&](int slot, bf16x8 (&vf)[4][2], unsigned vis) __attribute__((always_inline)) {
-        unsigned odd = 0;
+        unsigned top = 0;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
                 const u32x4 w = __builtin_bit_cast(u32x4, vf[t][u]);
-                odd |= nonfinite2(w[0]) | nonfinite2(w[1]) | nonfinite2(w[2]) | nonfinite2(w[3]);
+                top = top2(top2(top2(top2(top, w[0]), w[1]), w[2]), w[3]);
             }
-        if (__builtin_expect(__any(odd != 0), 0)) {
+        if (__builtin_expect(__any(nonfinite2(top) != 0), 0)) {
             const unsigned short *v = reinterpret_cast<const unsigned short *>(&v_lds[slot][0]);
             unsigned keys = 0;                           // this lane's: bit 8 u + e
 #pragma unroll
@@ -443,26 +443,18 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
         const int base = wk.w0 - wk.n_s + 2 * it0;
         const int f0 = __builtin_amdgcn_readfirstlane(max(((wk.n_s + 1) >> 1) - it0, ((((rb.lo1 + 15) >> 4) - base) + 1) >> 1));
         const int f1 = __builtin_amdgcn_readfirstlane(((rb.hi0 >> 4) - base) >> 1);
-        // exact pages: K of tile n + 1 is read while tile n's numerators are formed (69.2 -> 66.7 us for a pass of 2064 rows of 32
-        // heads; 4-bit pages have no registers for it: 277.8 -> 291.7 us)
+        // K of tile n + 1 is read while tile n's numerators are formed (69.2 -> 66.7 us for a pass of 2064 rows of 32 heads from
+        // exact pages, 263.5 -> 257.0 for a step of 8 sequences from 4-bit pages)
         bf16x8 k_next[8];
-        if constexpr (!KV4) k_frags(0, k_next);
+        k_frags(0, k_next);
         auto turn = [&](int n, int slot, Raw &x) __attribute__((always_inline)) {
             begin(n, slot);
             f32x16 s;
             bf16x8 vf[4][2];
             u32x4 pw[2];
-            if constexpr (KV4) {                         // (all eight reads before the first product: 278.0 -> 275.4 us)
-                bf16x8 kf[8];
-                k_frags(slot, kf);
-                __builtin_amdgcn_sched_barrier(0);
-                scores(kf, s);
-                v_frags(slot, vf);
-            } else {
-                scores(k_next, s);
-                v_frags(slot, vf);
-                k_frags((slot + 1) % RING, k_next);
-            }
+            scores(k_next, s);
+            v_frags(slot, vf);
+            k_frags((slot + 1) % RING, k_next);
             unsigned vis = 0;
             const bool masked = n < f0 || n >= f1;
             if (masked) {
@@ -472,7 +464,7 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
                 vis = cache ? cache_bits(rs, u0) | (cache_bits(rs, u1) << 16) : mask_bits(rs, u0) | (mask_bits(rs, u1) << 16);
                 const unsigned mine = vis >> (8 * lh);   // register e: key 8 lh + e % 8 of unit e / 8
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s[e] = ((mine >> ((e & 7) + 16 * (e >> 3))) & 1u) ? s[e] : -INFINITY;
+                for (int e = 0; e < 16; ++e) s[e] = seen_or_not(mine, (e & 7) + 16 * (e >> 3), s[e]);
             }
             // 4-bit pages: the softmax before the other wave's instructions (a prompt's pass on 12 heads 58.8 -> 57.8 us; exact pages lose 3 %)
             if constexpr (KV4) __builtin_amdgcn_s_setprio(1);

@@ -98,6 +98,16 @@ __device__ inline unsigned mask_bits(const RowSpan &s, int u) {
     return u < 0 ? 0u : bits16(s.ml - 16 * u, s.m1 - 16 * u) | bits16(s.m0 - 16 * u, s.ms - 16 * u);
 }
 
+// a score, or -inf where bit `bit` of `seen` is not set
+__device__ inline float seen_or_not(unsigned seen, int bit, float s) {
+    const unsigned m = (unsigned)((int)(seen << (31 - bit)) >> 31);
+    return __uint_as_float((__float_as_uint(s) & m) | (0xff800000u & ~m));
+}
+// the larger magnitudes of two pairs of bf16 values (as bits; of `top` magnitudes already)
+__device__ inline unsigned top2(unsigned top, unsigned x) {
+    typedef __attribute__((ext_vector_type(2))) unsigned short u16x2;
+    return __builtin_bit_cast(unsigned, __builtin_elementwise_max(__builtin_bit_cast(u16x2, top), __builtin_bit_cast(u16x2, x & 0x7fff7fffu)));
+}
 // of two bf16 values: bits where one is not finite; and zeros in the places of those
 __device__ inline unsigned nonfinite2(unsigned x) { return ((x & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
 __device__ inline unsigned nonfinite8(bf16x8 v) {        // the same as bits 0 .. 7 of eight values
