@@ -645,14 +645,14 @@ long long span_keys(const RowDesc &d, int rows, int window, int sinks, int max_p
 // 16 rows to a workgroup or 128: a wave that takes 16 rows starts and ends sooner, one that takes 32 reads its keys for twice as
 // many and shares them with three others.  What decides is the work in 16 rows by 32 keys, all sequences and heads together, from
 // exact pages in whole rounds of 256 workgroups, and that the rows fill enough of a workgroup's 128.  us with 16 and with 128 rows:
-//   4-bit pages   8 sequences of 1000 keys and 168 rows of a head (23 k): 32.8, 36.4;  1 of 8000 and 288 (36 k): 43.1, 41.9;
-//                 8 of 1000 and 288 (39 k): 50.5, 40.6;  1 of 8000 and 936 (30 k): 32.3, 44.3;  8 of 8000 and 48 (48 k): 45.2, 57.1
-//   exact pages   one round with a window of 1000 (8.4 k): 19.1, 25.9;  2000 (16 k): 28.1, 28.2;  3000 (24 k): 36.7, 30.9;
+//   4-bit pages   8 sequences of 1000 keys and 168 rows of a head (23 k): 32.7, 34.0;  8 of 8000 and 120 (32 k): 31.6, 34.5;
+//                 32 of 1000 and 252 (34 k): 41.9, 36.2;  8 of 1000 and 288 (39 k): 50.6, 36.6;  8 of 8000 and 48 (48 k): 44.3, 50.0
+//   exact pages   one round with a window of 1000 (8.4 k): 19.1, 25.9;  2000 (16 k): 27.6, 27.6;  3000 (24 k): 36.7, 29.6;
 //                 two rounds of 1000, 80 rows (16 k): 33.0, 26.8;  five, 288 rows (44 k): 73.1, 36.2
 static bool many_rows(int dtype, bool four, int F, long long wgs, long long keys) {
     if (dtype != TIDAR_BF16) return false;
     const long long its = (keys + 31) / 32;
-    if (four) return F > 64 && wgs * its > 36000;
+    if (four) return F > 64 && wgs * its > 33000;
     return F > 32 && (wgs > 256 ? (wgs + 255) / 256 * 256 : wgs) * its > 16200;
 }
 

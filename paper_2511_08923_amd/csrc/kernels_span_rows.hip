@@ -466,8 +466,6 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[e] = seen_or_not(mine, (e & 7) + 16 * (e >> 3), s[e]);
             }
-            // 4-bit pages: the softmax before the other wave's instructions (a prompt's pass on 12 heads 58.8 -> 57.8 us; exact pages lose 3 %)
-            if constexpr (KV4) __builtin_amdgcn_s_setprio(1);
             // the reference of a row, moved where the block's scores outgrow it (rare)
             float mx = -INFINITY;
 #pragma unroll
@@ -496,7 +494,6 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
                 pw[e >> 3][(e & 7) >> 1] = __builtin_bit_cast(unsigned, pk);
             }
             const bf16x8 pf[2] = {__builtin_bit_cast(bf16x8, pw[0]), __builtin_bit_cast(bf16x8, pw[1])};
-            if constexpr (KV4) __builtin_amdgcn_s_setprio(0);
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
