@@ -19,7 +19,6 @@
 // placement and join (890 TFLOP/s); 2064 rows over an exact window of 1024: 66 us.
 #include <algorithm>
 #include <cmath>
-#include <type_traits>
 
 #include "lds_dma.h"
 #include "span_device.h"
