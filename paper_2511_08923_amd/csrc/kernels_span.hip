@@ -526,8 +526,7 @@ __global__ __launch_bounds__(64 * W, 2) void span_attn_kernel(SpanArgs a) {
     for (int e = 0; e < PER; ++e) o[e] = 0.f;
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-        const float mw = m_lds[w][oq];
-        if (mw == -INFINITY) continue;                   // saw nothing
+        const float mw = m_lds[w][oq];                   // -inf: saw nothing, sums of 0, or NaN scores alone, sums of NaN
         const float wgt = mw == m ? 1.f : __builtin_amdgcn_exp2f(mw - m);
         sum += wgt * l_lds[w][oq];
 #pragma unroll
@@ -594,7 +593,7 @@ __global__ __launch_bounds__(64) void span_combine_kernel(const float *__restric
         }
 #pragma unroll
         for (int j = 0; j < J; ++j) {
-            if (s0 + 4 * j >= splits || m[j] == -INFINITY) continue;
+            if (s0 + 4 * j >= splits || l[j] == 0.f) continue;           // (a split of NaN scores alone has a maximum of -inf too)
             const float w = m[j] == m_all ? 1.f : __builtin_amdgcn_exp2f(m[j] - m_all);
             den += w * l[j];
 #pragma unroll

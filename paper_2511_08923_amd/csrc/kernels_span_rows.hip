@@ -562,8 +562,8 @@ __global__ __launch_bounds__(128) void span_rows_join_kernel(SpanArgs a) {
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const int s = min(s0 + j, S - 1);
-            ms[j] = s0 + j < S ? mp[(size_t)s * ROWS] : -INFINITY;
-            ls[j] = lp[(size_t)s * ROWS];
+            ms[j] = mp[(size_t)s * ROWS];
+            ls[j] = s0 + j < S ? lp[(size_t)s * ROWS] : 0.f;
             const f32x4 *op = partial_of(a, part + s, wave) + lane;
 #pragma unroll
             for (int t = 0; t < 4; ++t)
@@ -572,7 +572,7 @@ __global__ __launch_bounds__(128) void span_rows_join_kernel(SpanArgs a) {
         }
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-            if (ms[j] == -INFINITY) continue;            // saw nothing
+            if (ls[j] == 0.f) continue;                  // saw nothing (a piece of NaN scores alone has a maximum of -inf too)
             const float w = ms[j] == m ? 1.f : __builtin_amdgcn_exp2f(ms[j] - m);
             den += w * ls[j];
 #pragma unroll
