@@ -1,5 +1,7 @@
 // Kernels around the paged cache: page tables and slot maps from request lengths, rows of K and V into 4-bit pages and
 // back, and the placement of a windowed attention's new rows.  All of them move bytes; what bounds each stands with it.
+#include <algorithm>
+
 #include "kv4_format.h"
 #include "tidar_internal.h"
 
@@ -388,23 +390,38 @@ void launch_table_extend(int batch, const int32_t *prefix_len, const int32_t *n_
     table_extend_kernel<<<(batch + per_wg - 1) / per_wg, 256, 0, st>>>(a);
 }
 
-static RowArgs row_args(const Kv4View &kv, const int32_t *slots, int n_rows, const void *k, const void *v) {
-    return {kv, slots, n_rows, kv.hd % 8 == 0 && (((uintptr_t)k | (uintptr_t)v) & 15) == 0};
-}
-static dim3 row_grid(const Kv4View &kv, int n_rows) {
-    const size_t lanes = ((size_t)n_rows + 15) / 16 * 16 * kv.n_kv * 4 * kv4_blocks(kv.hd);
-    return dim3((unsigned)((lanes + 255) / 256));
+// A launch has fewer than 2^32 threads: `launch` gets rows [r0, r0 + n) in runs of at most 2^31 lanes, whole units of 16 rows but the last.
+template <class F>
+static void for_row_runs(const Kv4View &kv, const int32_t *slots, int n_rows, const void *k, const void *v, size_t esize, F launch) {
+    const size_t row_lanes = (size_t)kv.n_kv * 4 * kv4_blocks(kv.hd), row_bytes = (size_t)kv.n_kv * kv.hd * esize;
+    const size_t run = std::max<size_t>(16, ((size_t)1 << 31) / row_lanes & ~(size_t)15);
+    const int vec = kv.hd % 8 == 0 && (((uintptr_t)k | (uintptr_t)v) & 15) == 0;
+    for (size_t r0 = 0; r0 < (size_t)n_rows; r0 += run) {
+        const int n = (int)std::min<size_t>(run, n_rows - r0);
+        const size_t lanes = ((size_t)n + 15) / 16 * 16 * row_lanes;
+        launch(RowArgs{kv, slots + r0, n, vec}, dim3((unsigned)((lanes + 255) / 256)), r0 * row_bytes);
+    }
 }
 void launch_kv4_store(int dtype, const Kv4View &kv, const int32_t *slots, int n_rows, const void *k, const void *v,
                       hipStream_t st) {
-    const RowArgs a = row_args(kv, slots, n_rows, k, v);
-    if (dtype == TIDAR_BF16) kv4_store_kernel<<<row_grid(kv, n_rows), 256, 0, st>>>(a, (const bf16_t *)k, (const bf16_t *)v);
-    else kv4_store_kernel<<<row_grid(kv, n_rows), 256, 0, st>>>(a, (const float *)k, (const float *)v);
+    auto go = [&](auto t) {
+        typedef decltype(t) T;
+        for_row_runs(kv, slots, n_rows, k, v, sizeof(T), [&](const RowArgs &a, dim3 grid, size_t at) {
+            kv4_store_kernel<<<grid, 256, 0, st>>>(a, (const T *)((const char *)k + at), (const T *)((const char *)v + at));
+        });
+    };
+    if (dtype == TIDAR_BF16) go(bf16_t());
+    else go(float());
 }
 void launch_kv4_load(int dtype, const Kv4View &kv, const int32_t *slots, int n_rows, void *k, void *v, hipStream_t st) {
-    const RowArgs a = row_args(kv, slots, n_rows, k, v);
     const bool once = (size_t)n_rows * kv.n_kv * kv.hd * 4 > 32u << 20;
-    if (dtype == TIDAR_BF16 && once) kv4_load_kernel<bf16_t, true><<<row_grid(kv, n_rows), 256, 0, st>>>(a, (bf16_t *)k, (bf16_t *)v);
-    else if (dtype == TIDAR_BF16) kv4_load_kernel<bf16_t, false><<<row_grid(kv, n_rows), 256, 0, st>>>(a, (bf16_t *)k, (bf16_t *)v);
-    else kv4_load_kernel<float, false><<<row_grid(kv, n_rows), 256, 0, st>>>(a, (float *)k, (float *)v);
+    auto go = [&](auto kernel, auto t) {
+        typedef decltype(t) T;
+        for_row_runs(kv, slots, n_rows, k, v, sizeof(T), [&](const RowArgs &a, dim3 grid, size_t at) {
+            kernel<<<grid, 256, 0, st>>>(a, (T *)((char *)k + at), (T *)((char *)v + at));
+        });
+    };
+    if (dtype == TIDAR_BF16 && once) go(kv4_load_kernel<bf16_t, true>, bf16_t());
+    else if (dtype == TIDAR_BF16) go(kv4_load_kernel<bf16_t, false>, bf16_t());
+    else go(kv4_load_kernel<float, false>, float());
 }
