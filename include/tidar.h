@@ -392,7 +392,8 @@ tidar_status tidar_kv4_attention(tidar_ctx *ctx, const tidar_kv4_cache *kv, int3
                                  void *stream);
 
 /* Workspace of either for up to `batch` sequences with these rows, prefixes up to max_prefix_len and any window.  A call has at
- * most 2^18 rows per sequence and 2^26 rows of all query heads and sequences together (more: TIDAR_EINVAL). */
+ * most 2^18 rows per sequence, 2^26 rows of all query heads and sequences together and 2^22 K/V heads of all sequences together
+ * (more: TIDAR_EINVAL). */
 tidar_status tidar_attention_workspace_bytes(const tidar_ctx *ctx, int32_t batch, int32_t n_causal, int32_t n_blocks,
                                              int32_t block_len, int32_t max_prefix_len, size_t *bytes);
 

@@ -622,13 +622,16 @@ Kv4View layer_view4(const tidar_config &c, const tidar_kv4_cache *kv, int layer)
     return v;
 }
 
-// The rows of one attention call; false where they are not valid or too many (row indexes of a call are 32 bits).
+// The rows of one attention call; false where they are not valid or too many: row indexes of a call are 32 bits, and a launch has
+// fewer than 2^32 threads.  With at most 2^26 rows of all query heads and 2^22 (sequence, kv head) pairs there are below 2^23 tiles of
+// 16 rows, of 512 threads each, and below 2^24 units that new rows are placed in, of 256.
 bool span_rows(int batch, int32_t n_causal, int32_t n_blocks, int32_t block_len, int32_t cond0, const tidar_config &c,
                RowDesc *d) {
     if (n_causal < 1 || n_blocks < 0 || block_len < 1 || block_len > TIDAR_MAX_K || cond0 < 0) return false;
     if (n_blocks > 0 && (int64_t)cond0 + n_blocks - 1 > n_causal) return false;
     const int64_t rows = (int64_t)n_causal + (int64_t)n_blocks * block_len;
-    if (rows > (int64_t)1 << 18 || rows * batch * c.n_q_heads > (int64_t)1 << 26) return false;
+    if (rows > (int64_t)1 << 18 || rows * batch * c.n_q_heads > (int64_t)1 << 26 || (int64_t)batch * c.n_kv_heads > (int64_t)1 << 22)
+        return false;
     d->nc = n_causal;
     d->nb = n_blocks;
     d->bl = block_len;
