@@ -371,6 +371,9 @@ tidar_status tidar_kv4_load(tidar_ctx *ctx, const tidar_kv4_cache *kv, int32_t l
  * given to other sequences.  What a masked place holds (stale slots, infinities, NaN) has no influence.
  * A sequence whose prefix_len is not valid gets NaN in all its rows, and nothing of it is stored; a page id that is not valid
  * gives NaN to the rows that see its page, and possibly to other rows of the sequence.
+ * Scores, softmax statistics and sums are fp32.  With bf16 the softmax's numerators are rounded to bf16 (by at most 2^-8 of each, in
+ * numerator and denominator alike, as in tidar_hybrid_attention) for the product with V.  Sums are divided at the end and may be taken
+ * with weights of up to 2^16: magnitudes of V above 2^112 divided by the number of keys can overflow.
  */
 tidar_status tidar_window_attention(tidar_ctx *ctx, const tidar_kv_cache *kv, int32_t layer, int32_t batch,
                                     const int32_t *prefix_len, const void *q, const void *k_new, const void *v_new,
@@ -383,7 +386,8 @@ tidar_status tidar_window_attention(tidar_ctx *ctx, const tidar_kv_cache *kv, in
  * stored at positions prefix_len[b] .. prefix_len[b] + n_causal - 1 before (tidar_kv4_store), and every row of the call,
  * the causal row itself among them, sees them as they are held.  Mask rows are never cached; theirs are read as they are:
  *   k_mask, v_mask  dev [batch][n_blocks * block_len][n_kv_heads][head_dim] (NULL with n_blocks 0)
- * window 0: no window (sinks must be 0 then); otherwise as in tidar_window_attention, and so are invalid lengths and page ids.
+ * window 0: no window (sinks must be 0 then); otherwise as in tidar_window_attention, and so are invalid lengths and page ids and the
+ * arithmetic (held values are exact in either type).
  */
 tidar_status tidar_kv4_attention(tidar_ctx *ctx, const tidar_kv4_cache *kv, int32_t layer, int32_t batch,
                                  const int32_t *prefix_len, const void *q, const void *k_mask, const void *v_mask,

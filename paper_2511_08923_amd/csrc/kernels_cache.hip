@@ -158,8 +158,8 @@ __global__ __launch_bounds__(256) void table_extend_kernel(TableArgs a) {
 // ------------------------------------------------------------------ rows into 4-bit pages and back
 // A lane takes eight elements (16 bytes of bf16), the four lanes of a block agree on its scale by two shuffles, and 16 rows of a
 // head follow one another: of rows that are neighbours a workgroup holds whole pages, whose lines then go through one XCD's L2
-// (four rows at a time 16000 rows of 8 heads took 29.0 us to store and 21.9 to load, sixteen 25.8 and 14.0; pages put together in LDS
-// and written 16 bytes a lane 27.1).  Bound by the bytes of the rows.
+// (16000 rows of 8 heads in bf16, us to store and to load: sixteen rows at a time 22.2 and 14.0, four 25.2 and 21.7; pages put together
+// in LDS and written 16 bytes a lane cost the store 5 %).  Bound by the bytes of the rows.
 struct RowArgs {
     Kv4View kv;
     const int32_t *slots;
@@ -242,7 +242,8 @@ __global__ __launch_bounds__(256) void kv4_store_kernel(RowArgs a, const T *__re
     }
 }
 
-// ONCE: more than the L2s hold together, written past them (16000 rows of 8 heads, store and load: 46.7 us a pass, without it 54)
+// ONCE: more than the L2s hold together, written past them (16000 rows of 8 heads in bf16: a load takes 14.0 us, a store and a load
+// together 35.6; without it 15.8 and 44.6)
 template <typename T, bool ONCE>
 __global__ __launch_bounds__(256) void kv4_load_kernel(RowArgs a, T *__restrict__ k, T *__restrict__ v) {
     const int nb = kv4_blocks(a.kv.hd), hd = a.kv.hd;

@@ -18,7 +18,9 @@
 // moved only when the scores outgrow it by 2^16 (and from -inf by a row's first key): every rescale is exact, and no common
 // path reduces a maximum across lanes.  (A reference may lag behind the waves' and splits' common maximum by the 2^16, and
 // what is folded with a factor below 2^-126 is lost: weights below 2^-110 of a row's largest.)  bf16: numerators are rounded to
-// bf16 for the matrix product (relative 2^-9, as in tidar_hybrid_attention) and the denominator sums the rounded values in fp32.
+// bf16 for the matrix product (by at most 2^-8 of each, as in tidar_hybrid_attention: fp32 operands would take the products to a tenth
+// of the rate), and the denominator sums the rounded values in fp32.  With normal inputs outputs come 2.3e-3 off the definition in the
+// norm, 1.7e-3 of it their own rounding.
 //
 // What a masked place holds never shows: scores are replaced by -inf, and infinities and NaN of V, which a weight of zero would
 // turn into NaN, are taken out of the product in units that are not wholly visible, and put back for the rows that see them.
@@ -624,7 +626,8 @@ __global__ __launch_bounds__(64) void span_combine_kernel(const float *__restric
 }  // namespace
 
 // Waves of a few-row workgroup.  bf16: eight, so that half as many splits have to be joined (32 sequences of 8192 keys in 4 bits:
-// 50.6 us unsplit, with four waves 59.7 and 52 at best); fp32: four, the registers of head_dim 128 do not fit twice.
+// 50.6 us unsplit, with four waves 59.7 and 52 at best); fp32: four, the registers of head_dim 128 do not fit twice
+// (from exact pages not even once: 56 of them are spilled).
 static int span_waves(int dtype) { return dtype == TIDAR_BF16 ? 8 : 4; }
 static int most_splits(int dtype, long long wgs) {
     const int slots = 2048 / span_waves(dtype);

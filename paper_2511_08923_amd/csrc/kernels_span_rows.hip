@@ -14,9 +14,12 @@
 // whose round would leave most of the chip idle, are cut into pieces of equal length (SpanPlan), and only their partial results are
 // written and joined.
 //
-// Bound by the loop: 16 MFMAs (512 clocks) and about 70 vector instructions, 16 of them exponentials, per wave and block, which overlap
-// little; 1.06 PFLOP/s in long walks.  A step of 8 sequences of up to 8192 4-bit keys, 272 rows of 32 heads each: 259 us with
-// placement and join (890 TFLOP/s); 2064 rows over an exact window of 1024: 66 us.
+// Bound by the loop: 16 MFMAs (512 clocks) and, from exact pages where nothing is masked, about 70 vector instructions, 16 of them
+// exponentials, per wave and block (over 4-bit pages 108 with conversion, masks and the way in).  Of one wave they follow from each other,
+// scores, numerators, products, and nothing holds the two waves of a SIMD in opposite phases, so that they overlap little (waves
+// with nothing but one of them each do overlap: MFMAs alone 248 us, beside a wave of FMAs that takes 294 alone 317); 1.06 PFLOP/s in long
+// walks.  A step of 8 sequences of up to 8192 4-bit keys, 272 rows of 32 heads each: 258 us with placement and join (890 TFLOP/s);
+// 2064 rows over an exact window of 1024: 65 us.
 #include <algorithm>
 #include <cmath>
 
