@@ -373,7 +373,8 @@ tidar_status tidar_kv4_load(tidar_ctx *ctx, const tidar_kv4_cache *kv, int32_t l
  * gives NaN to the rows that see its page, and possibly to other rows of the sequence.
  * Scores, softmax statistics and sums are fp32.  With bf16 the softmax's numerators are rounded to bf16 (by at most 2^-8 of each, in
  * numerator and denominator alike, as in tidar_hybrid_attention) for the product with V.  Sums are divided at the end and may be taken
- * with weights of up to 2^16: magnitudes of V above 2^112 divided by the number of keys can overflow.
+ * with weights of up to 2^16: magnitudes of V above 2^112 divided by the number of keys can overflow.  With bf16, scores
+ * (q . k / sqrt(head_dim)) of a magnitude of 2^30 and more may give NaN, as in tidar_hybrid_attention.
  */
 tidar_status tidar_window_attention(tidar_ctx *ctx, const tidar_kv_cache *kv, int32_t layer, int32_t batch,
                                     const int32_t *prefix_len, const void *q, const void *k_new, const void *v_new,

@@ -80,10 +80,13 @@ __global__ __launch_bounds__(64 * W, 2) void span_attn_kernel(SpanArgs a) {
             if (row) qb[s] = *(const bf16x8 *)(qp + (KV4 ? 32 * kg + 8 * s : 32 * s + 8 * kg));
         }
     } else {
+        // (with the scale, so that the scores' distances from the reference are exact: times it afterwards they are off by 2^7 from
+        // 2^31 on, and a row may lose its largest numerator or get an infinite one)
+        const float to_log2 = kLog2e / sqrtf((float)hd);
 #pragma unroll
-        for (int s = 0; s < Q4; ++s) qf[s] = row && Q4 * kg + s < hd ? qp[Q4 * kg + s] : 0.f;
+        for (int s = 0; s < Q4; ++s) qf[s] = row && Q4 * kg + s < hd ? qp[Q4 * kg + s] * to_log2 : 0.f;
     }
-    const float scale = kLog2e / sqrtf((float)hd);
+    const float scale = BF ? kLog2e / sqrtf((float)hd) : 1.f;
     f32x4 acc[HT];
 #pragma unroll
     for (int t = 0; t < HT; ++t) acc[t] = (f32x4){0.f, 0.f, 0.f, 0.f};
