@@ -3,7 +3,7 @@ others, unless the two largest are as close as a sum of products in fp32 is off 
 each): such a row may take either, and only has to be finite.
 
 bf16 takes numerators as 2^(s * scale - m) with one rounding, whose error reaches 2^7 from s * scale = 2^31 on: magnitudes up to 2^30.
-fp32 has the factor in Q, and s - m is exact there at any size.
+fp32 scales the scores first, and the distance from m is exact then at any size.
 """
 import math
 
