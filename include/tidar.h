@@ -413,7 +413,8 @@ tidar_status tidar_attention_workspace_bytes(const tidar_ctx *ctx, int32_t batch
  * tidar_tree_commit puts those of the accepted path into it: a rejected draft needs no page.
  * Order of a step: tidar_tree_plan; per layer the projections and tidar_tree_attention; tidar_tree_accept; tidar_tree_commit.
  * A sequence whose row_start entries are not in order or run past n_rows, whose tree has more than 256 rows, a parent that is not
- * valid or a prefix_len below 0 (above 2^30) is reported as each call says, and does not affect the others.
+ * valid or a prefix_len below 0 (above 2^30) is reported as each call says, and does not affect the others.  Where entries that are not in order give
+ * the same row to two sequences, each with a range that is in order by itself, the later one's row_start is not valid.
  */
 
 /*
@@ -421,7 +422,8 @@ tidar_status tidar_attention_workspace_bytes(const tidar_ctx *ctx, int32_t batch
  *   prefix_len  dev int32 [batch]; row_start dev int32 [batch + 1]; parent dev int32 [n_rows]
  *   pos         dev int32 [n_rows] out: position id, prefix_len[b] + number of ancestors (for RoPE)
  *   ancestors   dev uint32 [n_rows][8] out, 16-byte aligned: bit j % 32 of word j / 32 = row j of the tree is this row or an ancestor of it
- * A sequence that is not valid gets pos -1 and no ancestors in all its rows.  Outputs may not overlap inputs (TIDAR_EINVAL).
+ * A sequence that is not valid gets pos -1 and no ancestors in its rows: all of them, or, where its row_start is not valid, those from its first row within the
+ * arrays up to the next one that another sequence has.  Outputs may not overlap inputs (TIDAR_EINVAL).
  */
 tidar_status tidar_tree_plan(tidar_ctx *ctx, int32_t batch, const int32_t *prefix_len, const int32_t *row_start, int32_t n_rows,
                              const int32_t *parent, int32_t *pos, uint32_t *ancestors, void *stream);

@@ -45,6 +45,7 @@ __global__ __launch_bounds__(64 * W, 2) void span_attn_kernel(SpanArgs a) {
     constexpr bool QUADS = !BF || KV4;                   // a lane's eight keys: two quads, or a run of eight
     __shared__ float red[W][16][HD + 4];
     __shared__ float m_lds[W][16], l_lds[W][16];
+    __shared__ int taken_lds[W];                         // a tree: whether its rows are another one's too, which stores them
     const SpanCall &c = a.c;
     const RowDesc &d = c.d;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -58,8 +59,10 @@ __global__ __launch_bounds__(64 * W, 2) void span_attn_kernel(SpanArgs a) {
     const int b = grp / n_kv, g = grp - b * n_kv;
     int R = d.R, row0 = b * d.R;                         // this sequence's rows, and the first of them
     if constexpr (TREE) {
-        R = tree_rows(c.row_start, c.n_rows, d.R, b, row0);
+        R = tree_range(c.row_start, c.n_rows, d.R, b, row0);
         if (tile * 16 >= a.group * R) return;
+        const bool taken = tree_taken(c.row_start, c.n_rows, d.R, b, row0, R, tid, 64 * W);
+        if (lane == 0) taken_lds[wave] = taken;
     }
     const int F = a.group * R;
     const int L_raw = c.prefix_len[d.seq_base + b];
@@ -576,6 +579,12 @@ __global__ __launch_bounds__(64 * W, 2) void span_attn_kernel(SpanArgs a) {
     constexpr int LANES = 4 * W, PER = HD / LANES;       // a row's threads, and the values of each
     const int oq = tid / LANES, od = (tid % LANES) * PER, of = tile * 16 + oq;
     if (of >= F) return;
+    if constexpr (TREE) {
+        int taken = 0;
+#pragma unroll
+        for (int w = 0; w < W; ++w) taken |= taken_lds[w];
+        if (taken) return;
+    }
     float m = m_lds[0][oq];
 #pragma unroll
     for (int w = 1; w < W; ++w) m = fmaxf(m, m_lds[w][oq]);

@@ -59,7 +59,7 @@ __device__ inline Place place_of(const SpanArgs &a, int n_kv, int item) {
     p.g = grp - p.b * n_kv;
     p.R = a.c.d.R;
     p.row0 = p.b * p.R;
-    if constexpr (TREE) p.R = tree_rows(a.c.row_start, a.c.n_rows, a.c.d.R, p.b, p.row0);
+    if constexpr (TREE) p.R = tree_range(a.c.row_start, a.c.n_rows, a.c.d.R, p.b, p.row0);      // (tree_taken: where rows are stored)
     const int F = a.group * p.R;
     p.f0 = span * a.span_rows + ((grp * spans + span) & 1 ? per_span - 1 - at : at) * ROWS;
     p.f1 = min(min(p.f0 + ROWS, (span + 1) * a.span_rows), F);
@@ -136,7 +136,7 @@ template <bool KV4, bool TREE>
 __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
     __shared__ __attribute__((aligned(16))) bf16_t k_lds[RING][TILE];
     __shared__ __attribute__((aligned(16))) bf16_t v_lds[RING][TILE];
-    __shared__ int bad_lds;
+    __shared__ int bad_lds, taken_lds[4];                // (taken: a tree whose rows are another one's too, which stores them)
     __shared__ __attribute__((aligned(16))) uint32_t tree_lds[TREE ? ROWS * kTreeWords : 4];      // who the rows see of their tree
     const SpanCall &c = a.c;
     const RowDesc &d = c.d;
@@ -220,6 +220,8 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
         u32x4 x = {0, 0, 0, 0};
         if (fr < pl.f1) x = *(const u32x4 *)(c.ancestors + ((size_t)pl.row0 + rr) * kTreeWords + 4 * (tid & 1));
         *(u32x4 *)(tree_lds + 4 * tid) = x;
+        const bool taken = tree_taken(c.row_start, c.n_rows, d.R, b, pl.row0, pl.R, tid, 256);
+        if (lane == 0) taken_lds[wave] = taken;
     }
     RowBounds rb;
     if constexpr (TREE) rb = tree_bounds(pl.R, L);
@@ -545,6 +547,7 @@ __global__ __launch_bounds__(256, 2) void span_rows_kernel(SpanArgs a) {
     if (bad) bad_lds = 1;
     __syncthreads();
     if (!here) return;
+    if (TREE && (taken_lds[0] | taken_lds[1] | taken_lds[2] | taken_lds[3])) return;
     float l = l_run;
     l += __shfl_xor(l, 32);
     if (bad_lds) {
@@ -581,7 +584,7 @@ __global__ __launch_bounds__(128) void span_rows_join_kernel(SpanArgs a) {
     const int tail = blockIdx.x >> 2, n_kv = KV4 ? c.kv4.n_kv : c.kv.n_kv;
     const Place pl = place_of<TREE>(a, n_kv, a.whole + tail);
     const int f = pl.f0 + wave * 32 + lq;
-    if (pl.f0 + wave * 32 >= pl.f1) return;
+    if (pl.f0 + wave * 32 >= pl.f1 || (TREE && tree_taken(c.row_start, c.n_rows, c.d.R, pl.b, pl.row0, pl.R, lane, 64))) return;
     const int part = a.pieces[2 * tail], S = a.pieces[2 * tail + 1];
     const float *mp = a.mpart + (size_t)part * ROWS + wave * 32 + lq, *lp = a.lpart + (size_t)part * ROWS + wave * 32 + lq;
     float m = -INFINITY;
@@ -660,7 +663,7 @@ __global__ __launch_bounds__(256) void tree_rows_prepare_kernel(SpanArgs a, cons
         __shared__ __attribute__((aligned(16))) bf16_t vt[16][HD + 2];
         const int at0 = blockIdx.x - first_tile, mt = at0 % n_mt, bg = at0 / n_mt, b = bg / n_kv, g = bg - b * n_kv;
         int row0;
-        const int R = tree_rows(c.row_start, c.n_rows, c.d.R, b, row0), n = R - 16 * mt;
+        const int R = tree_range(c.row_start, c.n_rows, c.d.R, b, row0), n = R - 16 * mt;
         if (n <= 0) return;
         typedef bf16x8 any_bf16x8 __attribute__((aligned(2)));
         const int r = tid >> 4, e = (tid & 15) * 8;
@@ -685,7 +688,7 @@ __global__ __launch_bounds__(256) void tree_rows_prepare_kernel(SpanArgs a, cons
     const int rest = groups * a.tiles - a.whole, lane = tid & 63, wave = tid >> 6;
     auto pieces_of = [&](int b, int &keys) {             // of a walk of sequence b, and the iterations of one
         int L, row0;
-        const int n = tree_rows(c.row_start, c.n_rows, c.d.R, b, row0);
+        const int n = tree_range(c.row_start, c.n_rows, c.d.R, b, row0);
         keys = 0;
         if (n == 0) return 0;
         if (!length_of(a, b, pps, L)) return 1;

@@ -14,6 +14,21 @@ __device__ inline void rows_within(const int32_t *row_start, int n_rows, int b, 
     e = min(max(row_start[b + 1], s), n_rows);
 }
 
+// The end of the rows from s on that no sequence but b has a range of (s itself, where one has): asked by a whole workgroup.
+__device__ inline int end_of_free(const int32_t *row_start, int n_rows, int b, int s, int e) {
+    __shared__ int end;
+    if (threadIdx.x == 0) end = e;
+    __syncthreads();
+    const int B = gridDim.x;
+    for (int x = threadIdx.x; x < B; x += 256) {
+        int s1;
+        const int m = tree_range(row_start, n_rows, TIDAR_MAX_TREE, x, s1);
+        if (x != b && m > 0 && s1 + m > s) atomicMin(&end, max(s1, s));
+    }
+    __syncthreads();
+    return end;
+}
+
 // A row's bits are its own and its parent's.  Every row starts with its own bit and its parent as the row to look up next; each
 // step adds that row's bits and goes on to the row that that one would look up, which is twice as far: eight steps for 256.
 __global__ __launch_bounds__(256) void tree_plan_kernel(const int32_t *__restrict__ prefix_len, const int32_t *__restrict__ row_start,
@@ -25,16 +40,18 @@ __global__ __launch_bounds__(256) void tree_plan_kernel(const int32_t *__restric
     int s, e;
     rows_within(row_start, n_rows, b, s, e);
     const int n = e - s;
-    const bool here = i < n;
-    bool bad = row_start[b] != s || row_start[b + 1] != e || n > TIDAR_MAX_TREE || L < 0 || L > (1 << 30);
+    const bool here = i < n, taken = tree_taken(row_start, n_rows, TIDAR_MAX_TREE, b, s, n, i & 63, 64);
+    const bool mine = row_start[b] == s && row_start[b + 1] == e && n <= TIDAR_MAX_TREE && !taken;       // (the same in all threads)
+    bool bad = !mine || L < 0 || L > (1 << 30);
     int p = -1;
     if (!bad && here) {
         p = parent[s + i];
         bad = p < -1 || p >= i;
     }
     if (__syncthreads_or(bad)) {
-        for (int r = i; r < n; r += 256) pos[s + r] = -1;
-        for (long long w = i; w < (long long)n * kTreeWords; w += 256) ancestors[(size_t)s * kTreeWords + w] = 0;
+        if (!mine) e = end_of_free(row_start, n_rows, b, s, e);          // (other workgroups write the others' rows)
+        for (int r = s + i; r < e; r += 256) pos[r] = -1;
+        for (size_t w = (size_t)s * kTreeWords + i; w < (size_t)e * kTreeWords; w += 256) ancestors[w] = 0;
         return;
     }
 #pragma unroll
@@ -84,6 +101,7 @@ __global__ __launch_bounds__(256) void tree_accept_kernel(AcceptArgs a) {
     const int n = e - s;
     const bool here = i < n;
     bool bad = a.row_start[b] != s || a.row_start[b + 1] != e || n < 1 || n > TIDAR_MAX_TREE || L < 0;
+    bad = tree_taken(a.row_start, a.n_rows, TIDAR_MAX_TREE, b, s, n, i, 256) || bad;        // (a wave's share of them: the workgroup asks together below)
     int p = -1;
     child[i] = TIDAR_MAX_TREE;
     if (!bad && here) {
