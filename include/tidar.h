@@ -506,7 +506,7 @@ tidar_status tidar_fp8_pack_weight(int32_t dtype, const void *src, int32_t rows,
 /*
  * out[M][N] (dev, out_dtype TIDAR_F32 or TIDAR_BF16) = a[M][K] (dev, config dtype) x weight (N rows, K cols)^T, both as they are held in 8 bits: the
  * rows of `a` are brought into that form by the call.  ws must hold tidar_fp8_gemm_workspace_bytes(M, N, K) bytes (0: sizes that are not
- * supported; beside the operands', more than 2^35 outputs).
+ * supported; beside the operands', more than 2^35 outputs), which also hold every call of fewer rows with the same N and K.
  */
 size_t       tidar_fp8_gemm_workspace_bytes(int32_t M, int32_t N, int32_t K);
 tidar_status tidar_fp8_gemm(tidar_ctx *ctx, const void *a, const void *w8, void *out, int32_t out_dtype, int32_t M, int32_t N, int32_t K,

@@ -370,12 +370,15 @@ void launch_tile(const Gemm8Args &g, const Gemm8Plan &p, float *part, hipStream_
 
 }  // namespace
 
-// Estimated time of the many-row kernel, us: its workgroups in rounds on 256 compute units (the last one, where units stand idle, counts
-// half of that: the others' clock rises), and the splits' partial sums out and back.  us of a chunk of 64 k, measured with every unit busy: wave
+// Estimated time of the many-row kernel, us, but for partial sums: its workgroups in rounds on 256 compute units (the last one, where units stand
+// idle, counts half of that: the others' clock rises).  us of a chunk of 64 k, measured with every unit busy: wave
 // tiles of 32 rows 1, 2, 3, 4 by two of 32 columns .22, .33, .40, .46, by four .42, .47, .58, .69.
-static double tile_time(const Gemm8Plan &p, int colblk, int M, int N) {
+static double tile_wg_time(int ra, int ca, int per, int splits) {          // of a workgroup
     static const double chunk_us[2][4] = {{0.22, 0.33, 0.40, 0.46}, {0.42, 0.47, 0.58, 0.69}};
-    auto wg = [&](int r) { return 2.5 + 2 * p.per * chunk_us[p.ca / 4][r - 1] + 0.35 * r * p.ca * (p.splits > 1 ? 2 : 1); };
+    return 2.5 + 2 * per * chunk_us[ca / 4][ra - 1] + 0.35 * ra * ca * (splits > 1 ? 2 : 1);
+}
+static double tile_time(const Gemm8Plan &p, int colblk) {
+    auto wg = [&](int r) { return tile_wg_time(r, p.ca, p.per, p.splits); };
     const long long nt = (long long)p.tall * colblk * p.splits, ns = (long long)p.shorts * colblk * p.splits;
     const double T = wg(p.ra), S = ns ? wg(p.ra - 1) : 0.0;
     // the tall ones in rounds, the short ones where there is room first
@@ -388,48 +391,79 @@ static double tile_time(const Gemm8Plan &p, int colblk, int M, int N) {
         left -= n[k];
         end = std::max(end, at[k]);
     }
-    const double even = std::max(T, (nt * T + ns * S) / 256.0);
-    return 0.5 * (end + even) + (p.splits > 1 ? 4.0 + (double)M * N * 4 * p.splits / 4.5e6 : 0.0);
+    return 0.5 * (end + std::max(T, (nt * T + ns * S) / 256.0));
 }
+static double part_time(int M, int N, int splits) { return 4.0 + (double)M * N * 4 * splits / 4.5e6; }      // partial sums, out and back
 
 static int few_tiles(int M) { return M <= 16 ? 1 : M <= 32 ? 2 : 4; }     // row tiles of a workgroup of few rows
 
-Gemm8Plan plan_gemm_fp8(int M, int N, int K) {
-    Gemm8Plan p = {};
-    const int nb = fp8_blocks(K), units = (M + 63) / 64;
-    p.splits = 1;
-    p.per = nb;
-    if (M <= 16) return p;
-    // few rows: what a compute unit takes in, at 52 GB/s, or the weights at 5 TB/s.  us with few and with many rows' kernel, conversion and all:
-    // 64 x 6144 x 4096 13.3, 14.3;  64 x 24576 x 4096 42, 26.8;  64 x 4096 x 12288 23.1, 19.0;  32 x 6144 x 4096 9.8, 13.5;  32 x 24576 x 4096 29, 26.2
-    const int mt = few_tiles(M), passes = (fp8_tiles(M) + mt - 1) / mt;
-    const double bytes = (double)N * nb * 128;
-    double best = M > 1 << 16 ? 1e30 : 1.5 + std::max((double)fp8_tiles(N) * passes * (mt + 1) * nb * 2048.0 / 256 / 52e3, bytes / 5e6);
-    for (int ca = 2; ca <= 4; ca += 2)
-        for (int ra = 1; ra <= 4 && ra <= units; ++ra) {
-            Gemm8Plan q = {};
-            const int passes = (units + ra - 1) / ra, colblk = (N + 64 * ca - 1) / (64 * ca);
-            q.ra = ra;
-            q.ca = ca;
-            q.tall = units - passes * (ra - 1);           // as even as they go
-            q.shorts = passes - q.tall;
-            if (q.tall <= 0) continue;
-            for (const int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
-                if (s > nb) break;
-                q.per = (nb + s - 1) / s;
-                q.splits = (nb + q.per - 1) / q.per;
-                if (q.splits != s) continue;
-                const double t = std::max(tile_time(q, colblk, M, N), bytes / 4.6e6 + 2.0);
-                if (t < best) {
-                    best = t;
-                    p = q;
+// The plans that there are for rows in `units` of 64, first that of few rows: what a compute unit takes in, at 52 GB/s, or the weights at 5
+// TB/s.  us with few and with many rows' kernel, conversion and all:
+// 64 x 6144 x 4096 13.3, 14.3;  64 x 24576 x 4096 42, 26.8;  64 x 4096 x 12288 23.1, 19.0;  32 x 6144 x 4096 9.8, 13.5;  32 x 24576 x 4096 29, 26.2
+struct Gemm8Plans {
+    int N, nb, n;
+    Gemm8Plan plan[2 * 4 * 12];
+    double us[2 * 4 * 12];
+    Gemm8Plans(int units, int N, int nb) : N(N), nb(nb), n(0) {
+        for (int ca = 2; ca <= 4; ca += 2)
+            for (int ra = 1; ra <= 4 && ra <= units; ++ra) {
+                Gemm8Plan q = {};
+                const int passes = (units + ra - 1) / ra, colblk = (N + 64 * ca - 1) / (64 * ca);
+                q.ra = ra;
+                q.ca = ca;
+                q.tall = units - passes * (ra - 1);       // as even as they go
+                q.shorts = passes - q.tall;
+                if (q.tall <= 0) continue;
+                for (const int s : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64}) {
+                    if (s > nb) break;
+                    q.per = (nb + s - 1) / s;
+                    q.splits = (nb + q.per - 1) / q.per;
+                    if (q.splits != s) continue;
+                    plan[n] = q;
+                    us[n++] = tile_time(q, colblk);
                 }
             }
+    }
+    Gemm8Plan best(int M) const {                         // for M rows, more than 16, of these units
+        Gemm8Plan p = {};
+        p.splits = 1;
+        p.per = nb;
+        const int mt = few_tiles(M), passes = (fp8_tiles(M) + mt - 1) / mt;
+        const double bytes = (double)N * nb * 128;
+        double best = M > 1 << 16 ? 1e30 : 1.5 + std::max((double)fp8_tiles(N) * passes * (mt + 1) * nb * 2048.0 / 256 / 52e3, bytes / 5e6);
+        for (int i = 0; i < n; ++i) {
+            const double t = std::max(us[i] + (plan[i].splits > 1 ? part_time(M, N, plan[i].splits) : 0.0), bytes / 4.6e6 + 2.0);
+            if (t < best) {
+                best = t;
+                p = plan[i];
+            }
         }
+        return p;
+    }
+};
+
+Gemm8Plan plan_gemm_fp8(int M, int N, int K) {
+    const int nb = fp8_blocks(K);
+    if (M > 16) return Gemm8Plans((M + 63) / 64, N, nb).best(M);
+    Gemm8Plan p = {};
+    p.splits = 1;
+    p.per = nb;
     return p;
 }
 size_t gemm_fp8_part_bytes(const Gemm8Plan &p, int M, int N) {
     return p.splits > 1 ? (size_t)p.splits * M * N * 4 : 0;
+}
+// The most of any count of rows up to M: fewer rows can have more splits.  A split saves at most an unsplit workgroup's time (the round that is
+// not full), so that no count is split from where its partial sums take longer on.
+size_t gemm_fp8_most_part_bytes(int M, int N, int K) {
+    const int nb = fp8_blocks(K);
+    size_t most = 0;
+    for (int m = 17; m <= M && part_time(m, N, 2) < tile_wg_time(4, 4, nb, 1);) {
+        const Gemm8Plans plans((m + 63) / 64, N, nb);
+        for (const int end = std::min((m + 63) / 64 * 64, M); m <= end; ++m)
+            most = std::max(most, gemm_fp8_part_bytes(plans.best(m), m, N));
+    }
+    return most;
 }
 
 void launch_fp8_pack(int dtype, const void *src, int rows, int K, unsigned char *dst, int dst_rows, int tile_off, int tile_stride,

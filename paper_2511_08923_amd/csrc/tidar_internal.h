@@ -433,6 +433,7 @@ struct Gemm8Plan {
 };
 Gemm8Plan plan_gemm_fp8(int M, int N, int K);
 size_t gemm_fp8_part_bytes(const Gemm8Plan &p, int M, int N);
+size_t gemm_fp8_most_part_bytes(int M, int N, int K);      // of M rows or fewer
 bool gemm_fp8_own_rows(int M, int N, int K);
 void launch_gemm_fp8_own(int dtype, const void *a, const unsigned char *w, void *out, int out_dtype, int M, int N, int K, hipStream_t st);
 void launch_gemm_fp8(const unsigned char *a, const unsigned char *w, void *out, int out_dtype, int M, int N, int K, const Gemm8Plan &p,

@@ -1407,7 +1407,7 @@ static bool fp8_gemm_ok(int32_t M, int32_t N, int32_t K) {
 }
 size_t tidar_fp8_gemm_workspace_bytes(int32_t M, int32_t N, int32_t K) {
     if (!fp8_gemm_ok(M, N, K)) return 0;
-    return align_up(fp8_bytes(M, K)) + align_up(gemm_fp8_part_bytes(plan_gemm_fp8(M, N, K), M, N));
+    return align_up(fp8_bytes(M, K)) + align_up(gemm_fp8_most_part_bytes(M, N, K));
 }
 
 tidar_status tidar_fp8_gemm(tidar_ctx *ctx, const void *a, const void *w8, void *out, int32_t out_dtype, int32_t M, int32_t N, int32_t K,
