@@ -45,14 +45,21 @@ __device__ inline void dma16_at(unsigned lds_addr, int voff, int4v desc, int sof
                      : "s"(lds_addr), "v"(voff), "s"(desc), "s"(soff), "n"(OFFSET)
                      : "memory", "m0");
 }
-// Load i < 4 of a run of tiles of 1 KiB that lie side by side in memory, from the descriptor's base, and in LDS, from lds_addr on.  The first
-// sets M0, the others rely on it: nothing between them may write it (only loads of this file do).
+// Load i < 4 of a run of tiles of 1 KiB that lie side by side in memory, from the descriptor's base, and in LDS, from lds_addr on.  (Each sets
+// M0 itself.  Left to the first of a run, whatever comes between the loads must not write it, which the compiler does not know: 2064 x 24576 x 4096
+// in 8 bits 181.0 us instead of 182.8.)
+template <int OFFSET>
+__device__ __attribute__((always_inline)) inline void dma16_run_at(unsigned lds_addr, int voff, int4v desc) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen offset:%3 lds"
+                 :
+                 : "s"(lds_addr), "v"(voff), "s"(desc), "n"(OFFSET)
+                 : "memory", "m0");
+}
 __device__ __attribute__((always_inline)) inline void dma16_run(unsigned lds_addr, int voff, int4v desc, int i) {
-    if (i == 0)
-        asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(lds_addr), "v"(voff), "s"(desc) : "memory", "m0");
-    else if (i == 1) asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:%2 lds" : : "v"(voff), "s"(desc), "n"(1024) : "memory");
-    else if (i == 2) asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:%2 lds" : : "v"(voff), "s"(desc), "n"(2 * 1024) : "memory");
-    else asm volatile("buffer_load_dwordx4 %0, %1, 0 offen offset:%2 lds" : : "v"(voff), "s"(desc), "n"(3 * 1024) : "memory");
+    if (i == 0) dma16_run_at<0>(lds_addr, voff, desc);
+    else if (i == 1) dma16_run_at<1024>(lds_addr, voff, desc);
+    else if (i == 2) dma16_run_at<2048>(lds_addr, voff, desc);
+    else dma16_run_at<3072>(lds_addr, voff, desc);
 }
 #pragma clang diagnostic pop
 // Tile i of tiles that lie side by side, 1 KiB each, in memory from soff and in LDS from lds_addr on: four share their base
