@@ -753,7 +753,10 @@ __global__ __launch_bounds__(256) void tree_rows_prepare_kernel(SpanArgs a, cons
     order[2 * tid] = before;
     order[2 * tid + 1] = before + x0;
     __syncthreads();
-    const int total = sums[0] + sums[1] + sums[2] + sums[3], half = min(total, 256 / a.tiles / 8 * 8);
+    const int total = sums[0] + sums[1] + sums[2] + sums[3];
+    // (more than 32 chunks to a head: eight pieces of each are more workgroups than units, and all go from long to short; there are few such pieces,
+    // and the other way round took as long: 7 trees of 256 rows of 32 heads over one of K/V, 4600 to 8000 keys, 185.2 and 185.6 us)
+    const int half = a.tiles > 32 ? total : min(total, 256 / a.tiles / 8 * 8);
 #pragma unroll
     for (int k = 0; k < 2; ++k)                          // (by sequence from here on: pieces, and where they begin)
         if (tid + 256 * k < c.B) len[tid + 256 * k] = pieces[k] | order[rank[k]] << 8;
