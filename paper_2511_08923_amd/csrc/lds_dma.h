@@ -57,9 +57,9 @@ __device__ __attribute__((always_inline)) inline void dma16_run_at(unsigned lds_
 }
 __device__ __attribute__((always_inline)) inline void dma16_run(unsigned lds_addr, int voff, int4v desc, int i) {
     if (i == 0) dma16_run_at<0>(lds_addr, voff, desc);
-    else if (i == 1) dma16_run_at<1024>(lds_addr, voff, desc);
-    else if (i == 2) dma16_run_at<2048>(lds_addr, voff, desc);
-    else dma16_run_at<3072>(lds_addr, voff, desc);
+    else if (i == 1) dma16_run_at<1 * 1024>(lds_addr, voff, desc);
+    else if (i == 2) dma16_run_at<2 * 1024>(lds_addr, voff, desc);
+    else dma16_run_at<3 * 1024>(lds_addr, voff, desc);
 }
 #pragma clang diagnostic pop
 // Tile i of tiles that lie side by side, 1 KiB each, in memory from soff and in LDS from lds_addr on: four share their base
