@@ -265,6 +265,13 @@ __global__ __launch_bounds__(256) void gemm8_tile_kernel(Gemm8Args g, int splits
 #pragma unroll
             for (int e = 0; e < 4; ++e) (f < CA ? wf[s][f < CA ? f : 0] : af[s][f < CA ? 0 : f - CA])[4 * k + e] = x[e];
         };
+        auto next_scales = [&]() __attribute__((always_inline)) {
+#pragma unroll
+            for (int f = 0; f < FRAGS; ++f) {
+                sc[f] = sc_next[f];
+                asm("" : "+v"(sc[f]));                   // (a word: taken for a byte across the loop, it is widened again in every pass)
+            }
+        };
         // Chunk c with fragment set s = c % 2.  The loads of chunk c + BUFS - 1 (whose place chunk c - 1 left) go out between the first
         // MFMAs, as far as they have not before; then chunk c + 1 has to have landed for everyone; then come the reads of its fragments, and the
         // first loads of chunk c + BUFS.  Spread evenly: four waves that ask at the same time wait for each other.
@@ -291,14 +298,11 @@ __global__ __launch_bounds__(256) void gemm8_tile_kernel(Gemm8Args g, int splits
 #pragma unroll
                 for (int k = FIRST * x / (N - FREE); k < FIRST * (x + 1) / (N - FREE); ++k) load(c + BUFS, k);
             }
-            if constexpr (s == 1)
-#pragma unroll
-                for (int f = 0; f < FRAGS; ++f) sc[f] = sc_next[f];
+            if constexpr (s == 1) next_scales();
         };
 #pragma unroll
         for (int r = 0; r < 3 * FRAGS; ++r) read(0, 0, r);
-#pragma unroll
-        for (int f = 0; f < FRAGS; ++f) sc[f] = sc_next[f];
+        next_scales();
         for (int c = 0; c < n_chunks; c += 2) {
             chunk(std::integral_constant<int, 0>(), c);
             chunk(std::integral_constant<int, 1>(), c + 1);
