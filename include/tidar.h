@@ -438,7 +438,8 @@ tidar_status tidar_tree_plan(tidar_ctx *ctx, int32_t batch, const int32_t *prefi
  *   max_prefix_len_hint  host bound of prefix_len
  * The cache is only read: keys below prefix_len from exact pages, or (tidar_kv4_tree_attention) as the 4-bit pages hold them; the tree's own rows
  * are read as they are.  A sequence whose prefix_len is not valid gets NaN in all its rows, and so do the rows of one that has a page id that is
- * not valid.  Arithmetic as in tidar_window_attention.  A workspace of tidar_tree_workspace_bytes also holds every call of fewer sequences, a
+ * not valid.  Arithmetic as in tidar_window_attention: scores, softmax statistics and sums are fp32; with bf16 the softmax's numerators are rounded to
+ * bf16, by at most 2^-8 of each, in numerator and denominator alike.  A workspace of tidar_tree_workspace_bytes also holds every call of fewer sequences, a
  * smaller bound of the rows and a smaller one of the prefixes.
  */
 tidar_status tidar_tree_workspace_bytes(const tidar_ctx *ctx, int32_t batch, int32_t max_nodes, int32_t max_prefix_len, size_t *bytes);

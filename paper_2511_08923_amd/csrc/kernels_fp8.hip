@@ -163,8 +163,9 @@ __global__ __launch_bounds__(64 * W, 6) void gemm8_few_kernel(Gemm8Args g, const
 // read, and the loads of the chunk after the next three go out, between this chunk's MFMAs.
 // out[m][n] = sum over blocks of K of 2^(ea + ew) (codes . codes): the MFMA takes both powers of two, so a block costs no instruction of its own.
 // 256 x 256 to a workgroup: 512 bytes from LDS for 131072 operations of a k, and 16 MFMAs of 64 clocks to each barrier; one wave to a
-// SIMD, since the sums take 256 registers.  Conversion of the rows and all: 2064 x 24576 x 4096 177 us, 2.35 PFLOP/s, 8192^3 445 us, 2.47 (the
-// kernel by itself 2.9).  Bound by the matrix cores at the clock they then run at (58 % busy at 1.99 GHz and 77 % at 1.82) and, with short K,
+// SIMD, since the sums take 256 registers (four registers are spilled around the loop, none in it).  Conversion of the rows and all, in captured
+// calls: 2064 x 24576 x 4096 179 us, 2.3 PFLOP/s, 8192^3 414 us, 2.66 (under a trace the kernel takes 436 by itself, at best 387).  Bound by the
+// matrix cores at the clock they then run at (58 % busy at 1.9 to 2.0 GHz and 77 % at 1.82) and, with short K,
 // by a workgroup's first loads and last stores, 2.3 and 6 us, which nothing else fills.
 // RA: row tiles of a wave in the first n_tall passes over the rows; the others, n_short, have one less (the workgroups of a launch are
 // started in order: short ones last fill up what the others leave).

@@ -19,7 +19,7 @@
 // scores, numerators, products, and nothing holds the two waves of a SIMD in opposite phases, so that they overlap little (waves
 // with nothing but one of them each do overlap: MFMAs alone 248 us, beside a wave of FMAs that takes 294 alone 317); 1.06 PFLOP/s in long
 // walks.  A step of 8 sequences of up to 8192 4-bit keys, 272 rows of 32 heads each: 258 us with placement and join (890 TFLOP/s);
-// 2064 rows over an exact window of 1024: 65 us.  Trees of 64 rows of 16 sequences, 4600 to 8200 exact keys, 32 heads: 129 us, the loop
+// 2064 rows over an exact window of 1024: 65 us.  Trees of 64 rows of 16 sequences, 4600 to 8200 exact keys, 32 heads: 126 to 132 us, the loop
 // by itself 111 to 123 (matrix cores busy 34 %); of 24 rows of 32 sequences over 4-bit pages 114, where a head's 96 rows leave one of the four waves idle.
 #include <algorithm>
 #include <cmath>

@@ -3,7 +3,7 @@
 // Sequence b's tree is rows [row_start[b], row_start[b + 1]) of the packed arrays, at most 256; a row's parent is the index, within
 // the tree, of a row that comes before it, or -1.  Both kernels take a workgroup per sequence and a tree in LDS; they are bound by
 // their launch and by dependent steps: a trip to memory for row_start, one for the rows, then LDS (one tree of 16 rows 3.1 and 2.9 us, 64 trees of
-// up to 64 rows 4.6 and 4.2).
+// up to 64 rows 4.7 and 4.2).
 #include "span_device.h"
 
 namespace {
